@@ -3,7 +3,9 @@ and its gradients, computed by hand-written HIP kernels behind the C ABI
 declared in ``include/gauss_sum.h`` (paper "Fast Gauss Sums via Flash
 Attention", Eq. 1 and the Sec. 3 gradient).
 
-``paper_2609_04910_amd.gauss_sum`` is the thin ctypes binding; importing this
-package does not load the GPU library.
+``paper_2609_04910_amd.gauss_sum`` is the thin ctypes binding,
+``paper_2609_04910_amd.attention`` that of softmax attention, the normalised sum
+(``include/gs_attention.h``); importing this package does not load the GPU
+libraries.
 """
-__all__ = ["gauss_sum", "workloads"]
+__all__ = ["attention", "gauss_sum", "workloads"]

@@ -1,0 +1,432 @@
+"""Thin ctypes binding of the C ABI in include/gs_attention.h: softmax attention,
+its gradients, and attention over a paged cache.
+
+Argument marshalling only, as in gauss_sum.py: every step of the computation
+runs in the HIP kernels of ``libgs_attention.so``, PyTorch provides device memory
+and the stream, there is no fallback, and errors are GaussSumError.
+
+Entry points (the C names without their ``gs_`` prefix):
+  attention_fwd(q, k, v, ...)                        -> out, lse
+  attention_bwd(q, k, v, out, lse, dout, ...)        -> dq, dk, dv
+  attention_append(k, v, k_pages, v_pages, page_table, seq_lens, ...)
+  attention_paged(q, k_pages, v_pages, page_table, seq_lens, ...) -> out
+  attention_bwd_workspace_size / attention_paged_workspace_size
+and ``attention(q, k, v, ...)`` is the forward call under autograd.
+
+Layouts.  Dense: q is B x M x Hq x D, k is B x N x Hkv x D, v is B x N x Hkv x C,
+with q_lens / k_lens (int32, B) the rows in use of each sequence where not all
+are.  Packed, with q_offsets / k_offsets (int32, B + 1; k_offsets defaults to
+q_offsets): q is T x Hq x D, k and v are S x Hkv x (D, C), the sequences one
+behind the other.  Any strides with contiguous columns; Hq a multiple of Hkv;
+fp16 or bf16, results in the inputs' dtype, lse (log sum exp of the scores) in
+fp32 as B x Hq x M or Hq x T.
+
+Rows that belong to no sequence are 0 (lse: -inf) in results allocated here and
+left as they were in the caller's own (out=, lse=).
+"""
+import ctypes
+import os
+
+from . import gauss_sum as gs
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+LIB_PATH = os.path.join(HERE, "libgs_attention.so")
+EXPORTED = ("gs_attention_fwd", "gs_attention_fwd_workspace_size", "gs_attention_bwd",
+            "gs_attention_bwd_workspace_size", "gs_attention_paged", "gs_attention_paged_workspace_size",
+            "gs_attention_append")
+REST_OUT, REST_LSE = 1, 2  # GS_ATTENTION_REST_OUT, GS_ATTENTION_REST_LSE
+
+
+class Problem(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("M", ctypes.c_int64), ("N", ctypes.c_int64), ("Hq", ctypes.c_int64),
+                ("Hkv", ctypes.c_int64), ("D", ctypes.c_int64), ("C", ctypes.c_int64), ("window", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("packed", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("zero_rest", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class Array(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k", Array), ("v", Array), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("table_width", ctypes.c_int64), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
+
+
+_lib = None
+
+
+def load(path=LIB_PATH, torch_runtime=True):
+    """Load libgs_attention.so (built in-tree by ``__graft_entry__.build()``); torch
+    first, as in gauss_sum.load."""
+    global _lib
+    if _lib is not None and path == LIB_PATH:
+        return _lib
+    if not os.path.exists(path):
+        raise RuntimeError("HIP library %s is missing: run __graft_entry__.build() first" % path)
+    if torch_runtime:
+        import torch  # noqa: F401
+    lib = ctypes.CDLL(path)
+    vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+    # structures are passed as byref(...): plain pointers keep the calls short
+    lib.gs_attention_fwd.argtypes = [vp] * 9 + [vp, sz, vp]
+    lib.gs_attention_bwd.argtypes = [vp] * 13 + [vp, sz, vp]
+    lib.gs_attention_paged.argtypes = [vp] * 6 + [vp, sz, vp]
+    lib.gs_attention_append.argtypes = [vp] * 6
+    lib.gs_attention_fwd_workspace_size.argtypes = [vp]
+    lib.gs_attention_bwd_workspace_size.argtypes = [vp, i32, i32, i32]
+    lib.gs_attention_paged_workspace_size.argtypes = [vp, vp]
+    for name in EXPORTED:
+        getattr(lib, name).restype = sz if name.endswith("_size") else i32
+    if path == LIB_PATH:
+        _lib = lib
+    return lib
+
+
+def _array(t, packed):
+    if t is None:
+        return None
+    s = t.stride()
+    if packed:
+        return Array(t.data_ptr(), 0, s[0], s[1])
+    return Array(t.data_ptr(), s[0], s[1], s[2])
+
+
+def _check_columns(name, t, dims):
+    if t.dim() != dims:
+        raise ValueError("%s must have %d dimensions, got %d" % (name, dims, t.dim()))
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("the columns of %s must be contiguous" % name)
+
+
+def _check_index(name, t, n, device):
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32:
+        raise TypeError("%s must be an int32 tensor" % name)
+    if t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous 1-d tensor%s, got %s"
+                         % (name, "" if n is None else " of %d" % n, tuple(t.shape)))
+    if t.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+
+
+def _scale(scale, D):
+    return D ** -0.5 if scale is None else float(scale)
+
+
+def _dtype(*named):
+    """The one dtype of the tensors: fp16 or bf16."""
+    code = gs._dtype_code(named[0][1].dtype)
+    if code == gs.GS_F32:
+        raise TypeError("%s must be float16 or bfloat16" % named[0][0])
+    for name, t in named[1:]:
+        if t.dtype != named[0][1].dtype:
+            raise TypeError("%s and %s must share a dtype" % (named[0][0], name))
+    return code
+
+
+def _check_gpu(*named):
+    device = named[0][1].device
+    for name, t in named:
+        if not t.is_cuda:
+            raise ValueError("%s must be a GPU tensor" % name)
+        if t.device != device:
+            raise ValueError("%s must be on %s" % (name, device))
+
+
+class _Call:
+    """Checked shapes of a forward or backward call."""
+
+    def __init__(self, q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens):
+        packed = q_offsets is not None
+        if k_offsets is not None and not packed:
+            raise ValueError("k_offsets needs q_offsets")
+        if packed and (q_lens is not None or k_lens is not None):
+            raise ValueError("q_lens / k_lens are for dense sequences, q_offsets / k_offsets for packed ones")
+        dims = 3 if packed else 4
+        for name, t in (("q", q), ("k", k), ("v", v)):
+            _check_columns(name, t, dims)
+        Hq, D = q.shape[-2:]
+        Hkv, C = v.shape[-2:]
+        if k.shape[-2] != Hkv or k.shape[-1] != D or k.shape[:-2] != v.shape[:-2]:
+            raise ValueError("k must be %s (rows and heads of v, columns of q), got %s"
+                             % ("x".join(map(str, v.shape[:-1] + (D,))), tuple(k.shape)))
+        if Hkv < 1 or Hq % Hkv or Hq == 0:
+            raise ValueError("%d query heads over %d key heads: must be a multiple" % (Hq, Hkv))
+        if not packed and q.shape[0] != k.shape[0]:
+            raise ValueError("q has %d sequences, k has %d" % (q.shape[0], k.shape[0]))
+        if window < 0 or (window and not causal):
+            raise ValueError("window must be 0, or positive with causal")
+        code = _dtype(("q", q), ("k", k), ("v", v))
+        if packed:
+            if k_offsets is None:
+                k_offsets = q_offsets
+            _check_index("q_offsets", q_offsets, None, q.device)
+            if q_offsets.shape[0] < 1:
+                raise ValueError("q_offsets must hold one number more than there are sequences")
+            _check_index("k_offsets", k_offsets, q_offsets.shape[0], q.device)
+            B, M, N = q_offsets.shape[0] - 1, q.shape[0], k.shape[0]
+            self.index = (q_offsets, k_offsets)
+            self.lse_shape = (Hq, M)
+        else:
+            B, M, N = q.shape[0], q.shape[1], k.shape[1]
+            for name, t in (("q_lens", q_lens), ("k_lens", k_lens)):
+                if t is not None:
+                    _check_index(name, t, B, q.device)
+            self.index = (q_lens, k_lens)
+            self.lse_shape = (B, Hq, M)
+        _check_gpu(("q", q), ("k", k), ("v", v))
+        self.packed = packed
+        self.out_shape = q.shape[:-1] + (C,)
+        self.problem = Problem(B, M, N, Hq, Hkv, D, C, int(window), code, int(packed), int(bool(causal)), 0,
+                               _scale(scale, D))
+
+
+def _launch(name, device, stream, *args):
+    """The library call on the tensors' device and the given (or its current) stream."""
+    import torch
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            st = getattr(load(), name)(*args, gs._stream(stream))
+    else:
+        st = getattr(load(), name)(*args, gs._stream(stream))
+    if st != 0:
+        raise gs.GaussSumError(st, name)
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def _check_out(t, name, shape, dtype, device):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a tensor" % name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, "x".join(map(str, shape)), tuple(t.shape)))
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+
+
+def _check_like_out(t, name, c, q):
+    _check_out(t, name, c.out_shape, q.dtype, q.device)
+    _check_columns(name, t, len(c.out_shape))
+
+
+def _fwd(c, q, k, v, out, lse, low, stream):
+    import torch
+    rest = 0
+    if out is None:
+        rest = REST_OUT
+        out = torch.empty(c.out_shape, dtype=q.dtype, device=q.device)
+    else:
+        _check_like_out(out, "out", c, q)
+    if lse is None:
+        lse = torch.empty(c.lse_shape, dtype=torch.float32, device=q.device)
+        rest |= REST_LSE
+    else:
+        gs._check_tensor(lse, "lse", c.lse_shape, q.device, torch.float32)
+    c.problem.zero_rest = rest
+    _launch("gs_attention_fwd", q.device, stream, _ref(c.problem), _ref(_array(q, c.packed)),
+            _ref(_array(k, c.packed)), _ref(_array(v, c.packed)), gs._ptr(c.index[0]), gs._ptr(c.index[1]),
+            _ref(_array(out, c.packed)), _ref(_array(low, c.packed)), gs._ptr(lse), None, 0)
+    gs._keep_alive(stream, out, lse)
+    return out, lse
+
+
+def attention_fwd(q, k, v, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None, q_lens=None,
+                  k_lens=None, out=None, lse=None, low=None, stream=None):
+    """(out, lse): out_m = sum_n w_mn v_n / sum_n w_mn with w_mn = exp(scale q_m.k_n) over the
+    keys that row m sees, lse_m = log sum_n w_mn.
+
+    scale defaults to D ** -0.5.  causal: row i of qn sees the keys j <= i + kn - qn of its
+    sequence's kn; window > 0 (with causal): only the last `window` of them.  A row that sees
+    nothing gives out = 0 and lse = -inf.  low: a tensor like out that receives what the rounding
+    of out leaves (out - rounded), which attention_bwd can use."""
+    c = _Call(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+    if low is not None:
+        _check_like_out(low, "low", c, q)
+    return _fwd(c, q, k, v, out, lse, low, stream)
+
+
+def attention_bwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed=False,
+                                 want_dq=True, want_dk=True, want_dv=True):
+    """Workspace bytes of attention_bwd (packed: M and N are the rows of all sequences)."""
+    p = Problem(B, M, N, Hq, Hkv, D, C, 0, dtype, int(packed), 0, 0, 1.0)
+    return int(load().gs_attention_bwd_workspace_size(_ref(p), int(bool(want_dq)), int(bool(want_dk)),
+                                                      int(bool(want_dv))))
+
+
+def _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream):
+    import torch
+    for name, t in (("out", out), ("dout", dout), ("low", low)):
+        if name != "low" or t is not None:
+            _check_like_out(t, name, c, q)
+    gs._check_tensor(lse, "lse", c.lse_shape, q.device, torch.float32)
+    grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if w else None
+             for t, w in zip((q, k, v), want)]
+    c.problem.zero_rest = REST_OUT
+    need = int(load().gs_attention_bwd_workspace_size(_ref(c.problem), *(int(bool(w)) for w in want)))
+    workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
+    _launch("gs_attention_bwd", q.device, stream, _ref(c.problem), _ref(_array(q, c.packed)),
+            _ref(_array(k, c.packed)), _ref(_array(v, c.packed)), gs._ptr(c.index[0]), gs._ptr(c.index[1]),
+            _ref(_array(out, c.packed)), _ref(_array(low, c.packed)), gs._ptr(lse), _ref(_array(dout, c.packed)),
+            *(_ref(_array(g, c.packed)) for g in grads), gs._ptr(workspace), wbytes)
+    gs._keep_alive(stream, workspace, *grads)
+    return tuple(grads)
+
+
+def attention_bwd(q, k, v, out, lse, dout, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None,
+                  q_lens=None, k_lens=None, want=(True, True, True), low=None, workspace=None, stream=None):
+    """(dq, dk, dv) of L = sum <dout, out> for the out, lse and (optional) low of attention_fwd with the
+    same arguments; None where not wanted.  dk and dv are summed over the query heads that share a key
+    head."""
+    c = _Call(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+    return _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream)
+
+
+def _make_autograd():
+    import torch
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, call):
+            low = torch.empty(call.out_shape, dtype=q.dtype, device=q.device) if any(ctx.needs_input_grad) else None
+            out, lse = _fwd(call, q, k, v, None, None, low, None)
+            ctx.save_for_backward(q, k, v, out, lse, low, *(t for t in call.index if t is not None))
+            ctx.call = call
+            return out
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, g):
+            q, k, v, out, lse, low = ctx.saved_tensors[:6]
+            want = ctx.needs_input_grad[:3]
+            if not any(want):
+                return None, None, None, None
+            if g.shape[-1] > 1 and g.stride(-1) != 1:
+                g = g.contiguous()
+            return _bwd(ctx.call, q, k, v, out, lse, g, want, low, None, None) + (None,)
+
+    return Attention
+
+
+_autograd = None
+
+
+def attention(q, k, v, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None, q_lens=None, k_lens=None):
+    """attention_fwd under autograd: out, with gradients for q, k and v (arguments as there)."""
+    global _autograd
+    if _autograd is None:
+        _autograd = _make_autograd()
+    c = _Call(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+    return _autograd.apply(q, k, v, c)
+
+
+def _cache_call(x, name, k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window, scale):
+    """(problem, cache, packed) of a call on T x H x width rows x."""
+    import torch
+    for n, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        _check_columns(n, t, 4)
+    Hkv = v_pages.shape[2]
+    if k_pages.shape[:3] != v_pages.shape[:3] or k_pages.shape[3] != D or v_pages.shape[3] != C:
+        raise ValueError("k_pages must be pages x page_size x Hkv x %d and v_pages the same x %d, got %s and %s"
+                         % (D, C, tuple(k_pages.shape), tuple(v_pages.shape)))
+    if k_pages.shape[1] < 1:
+        raise ValueError("pages must hold at least one row")
+    if Hkv < 1 or Hq % Hkv or Hq == 0:
+        raise ValueError("%d query heads over %d key heads: must be a multiple" % (Hq, Hkv))
+    if not isinstance(page_table, torch.Tensor) or page_table.dtype != torch.int32:
+        raise TypeError("page_table must be an int32 tensor")
+    if page_table.dim() != 2 or not page_table.is_contiguous():
+        raise ValueError("page_table must be a contiguous sequences x pages tensor")
+    if page_table.device != x.device:
+        raise ValueError("page_table must be on %s" % x.device)
+    B, T = page_table.shape[0], x.shape[0]
+    _check_index("seq_lens", seq_lens, B, x.device)
+    if q_offsets is not None:
+        _check_index("q_offsets", q_offsets, B + 1, x.device)
+        M = T
+    else:
+        if (T % B if B else T):
+            raise ValueError("%d rows of %s for %d sequences: give q_offsets" % (T, name, B))
+        M = T // B if B else 0
+    if window < 0:
+        raise ValueError("window must not be negative")
+    p = Problem(B, M, 0, Hq, Hkv, D, C, int(window), code, int(q_offsets is not None), 1, 0, scale)
+    cache = Cache(_array(k_pages, False), _array(v_pages, False), k_pages.shape[0], k_pages.shape[1],
+                  page_table.shape[1], page_table.data_ptr(), seq_lens.data_ptr())
+    return p, cache
+
+
+def _rows(t, p):
+    """T x H x width rows: packed, or M of every sequence."""
+    s = t.stride()
+    return Array(t.data_ptr(), 0 if p.packed else p.M * s[0], s[0], s[1])
+
+
+def attention_append(k, v, k_pages, v_pages, page_table, seq_lens, q_offsets=None, stream=None):
+    """Writes the keys k (T x Hkv x D) and values v (T x Hkv x C) of new tokens into the pages of
+    a cache, pages x page_size x Hkv x (D, C): token i of the qn new ones of sequence b goes to
+    position seq_lens[b] - qn + i, which is row position % page_size of page
+    page_table[b, position // page_size].  seq_lens (int32, B) counts the new tokens.  The T rows are
+    T / B of every sequence, or as q_offsets (int32, B + 1) says.  Positions outside the table
+    and page numbers outside the cache are passed over."""
+    _check_columns("k", k, 3)
+    _check_columns("v", v, 3)
+    if k.shape[:2] != v.shape[:2]:
+        raise ValueError("k and v must share rows and heads, got %s and %s" % (tuple(k.shape), tuple(v.shape)))
+    code = _dtype(("k", k), ("v", v), ("k_pages", k_pages), ("v_pages", v_pages))
+    H = k.shape[1]
+    p, cache = _cache_call(k, "k", k_pages, v_pages, page_table, seq_lens, q_offsets, H, k.shape[2], v.shape[2],
+                           code, 0, 1.0)
+    if p.Hkv != H:
+        raise ValueError("k has %d heads, the pages have %d" % (H, p.Hkv))
+    _check_gpu(("k", k), ("v", v), ("k_pages", k_pages), ("v_pages", v_pages))
+    _launch("gs_attention_append", k.device, stream, _ref(p), _ref(_rows(k, p)), _ref(_rows(v, p)), _ref(cache),
+            gs._ptr(q_offsets))
+
+
+def attention_paged_workspace_size(B, M, Hq, Hkv, D, C, page_size, table_width, dtype=gs.GS_F16, packed=False):
+    """Workspace bytes of attention_paged (M: tokens of a sequence; packed: of all sequences)."""
+    p = Problem(B, M, 0, Hq, Hkv, D, C, 0, dtype, int(packed), 1, 0, 1.0)
+    cache = Cache(Array(), Array(), 0, page_size, table_width, None, None)
+    return int(load().gs_attention_paged_workspace_size(_ref(p), _ref(cache)))
+
+
+def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, scale=None, window=0, out=None,
+                    return_lse=False, workspace=None, stream=None):
+    """Attention of a chunk of new tokens (or one) of every sequence, q: T x Hq x D, over a paged
+    cache that holds their keys and values already (attention_append; arguments as there):
+    token i of the qn new ones of sequence b sees the keys up to its own position,
+    seq_lens[b] - qn + i, with window > 0 the last `window` of them.  Returns out (T x Hq x C), or
+    (out, lse) with lse Hq x T.  A row that sees a key whose page number lies outside the cache is NaN."""
+    import torch
+    _check_columns("q", q, 3)
+    if not (isinstance(v_pages, torch.Tensor) and v_pages.dim() == 4):
+        raise ValueError("v_pages must have 4 dimensions")
+    code = _dtype(("q", q), ("k_pages", k_pages), ("v_pages", v_pages))
+    T, Hq, D = q.shape
+    C = v_pages.shape[3]
+    p, cache = _cache_call(q, "q", k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window,
+                           _scale(scale, D))
+    _check_gpu(("q", q), ("k_pages", k_pages), ("v_pages", v_pages))
+    if out is None:
+        p.zero_rest = REST_OUT
+        out = torch.empty((T, Hq, C), dtype=q.dtype, device=q.device)
+    else:
+        _check_out(out, "out", (T, Hq, C), q.dtype, q.device)
+        _check_columns("out", out, 3)
+    lse = None
+    if return_lse:
+        lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
+        p.zero_rest |= REST_LSE
+    need = int(load().gs_attention_paged_workspace_size(_ref(p), _ref(cache)))
+    workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
+    _launch("gs_attention_paged", q.device, stream, _ref(p), _ref(_rows(q, p)), _ref(cache), gs._ptr(q_offsets),
+            _ref(_rows(out, p)), gs._ptr(lse), gs._ptr(workspace), wbytes)
+    gs._keep_alive(stream, out, lse, workspace)
+    return (out, lse) if return_lse else out

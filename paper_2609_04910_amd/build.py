@@ -1,6 +1,7 @@
 """Build the gfx950 HIP libraries in-tree (hipcc, no JIT cache): libgauss_sum.so
-(the Gauss-sum kernels and their C ABI) and libgs_peaks.so (the rate
-calibration kernels the benchmark measures the device's own rates with).
+(the Gauss-sum kernels and their C ABI), libgs_attention.so (softmax attention)
+and libgs_peaks.so (the rate calibration kernels the benchmark measures the
+device's own rates with).
 
 Flags: -O3 for gfx950 only; packed fp32 instructions are disabled in the
 device code (-Xclang -target-feature -Xclang -packed-fp32-ops).
@@ -15,6 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "gauss_sum.hip")
 LIB = os.path.join(HERE, "libgauss_sum.so")
+ATTENTION_SRC = os.path.join(HERE, "csrc", "gs_attention.hip")
+ATTENTION_LIB = os.path.join(HERE, "libgs_attention.so")
 PEAKS_SRC = os.path.join(HERE, "peaks", "gs_peaks.hip")
 PEAKS_LIB = os.path.join(HERE, "libgs_peaks.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -31,9 +34,11 @@ FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
-    """Compile csrc/gauss_sum.hip into libgauss_sum.so and peaks/gs_peaks.hip
-    into libgs_peaks.so; returns the path of libgauss_sum.so."""
+    """Compile csrc/gauss_sum.hip into libgauss_sum.so, csrc/gs_attention.hip
+    into libgs_attention.so and peaks/gs_peaks.hip into libgs_peaks.so; returns
+    the path of libgauss_sum.so."""
     compile_one(PEAKS_SRC, PEAKS_LIB, verbose)
+    compile_parts(ATTENTION_SRC, ATTENTION_LIB, verbose)
     return compile_parts(SRC, LIB, verbose)
 
 
@@ -78,7 +83,7 @@ def compile_one(src: str, lib: str, verbose: bool) -> str:
 def sources():
     d = os.path.join(HERE, "csrc")
     return [os.path.join(d, f) for f in sorted(os.listdir(d))] + [
-        os.path.join(ROOT, "include", "gauss_sum.h")]
+        os.path.join(ROOT, "include", "gauss_sum.h"), os.path.join(ROOT, "include", "gs_attention.h")]
 
 
 if __name__ == "__main__":

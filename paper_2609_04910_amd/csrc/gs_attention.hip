@@ -1,0 +1,514 @@
+// gs_attention.hip -- host side and kernel instances of softmax attention
+// (include/gs_attention.h).
+//
+// Compiled as one unit (no GS_PART) or, in parallel, as GS_PARTS + 1 units: part 0
+// is the host side and the kernels that do not depend on the dtype's width, parts
+// 1 .. GS_PARTS one dtype and padded width each.
+#include "gs_attention.h"
+
+#include <type_traits>
+
+#include "gs_attn_bwd.h"
+#include "gs_attn_fwd.h"
+
+#define GS_PARTS 6
+#ifndef GS_PART
+#define GS_PART -1
+#endif
+#if GS_PART <= 0
+#include "gs_attn_append.h"
+#endif
+
+namespace gs {
+
+// Rows of a workgroup's waves: NQ query tiles of 16 a wave (NT column tiles in the
+// backward passes).
+constexpr int kAttnWaves = 4;
+constexpr int attn_nq(int DP) { return 2; }
+constexpr int attn_nt(int DP, bool KV) { return DP == 256 ? 1 : 2; }
+
+constexpr int attn_fwd_rows(int DP) { return 16 * kAttnWaves * attn_nq(DP); }
+constexpr int attn_bwd_cols(int DP, bool KV) { return 16 * kAttnWaves * attn_nt(DP, KV); }
+
+template <typename K, typename A>
+hipError_t launch(K kernel, int64_t grid, int threads, const A& args, hipStream_t st) {
+  void* p[1] = {const_cast<A*>(&args)};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(threads), p, 0, st);
+}
+
+template <typename T, int DP>
+hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int64_t grid, hipStream_t st);
+template <typename T, int DP>
+hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st);
+
+#if GS_PART != 0
+template <typename T, int DP>
+hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int64_t grid, hipStream_t st) {
+  return paged ? launch(&k_attn_fwd<T, DP, attn_nq(DP), kAttnWaves, true>, grid, 64 * kAttnWaves, a, st)
+               : launch(&k_attn_fwd<T, DP, attn_nq(DP), kAttnWaves, false>, grid, 64 * kAttnWaves, a, st);
+}
+template <typename T, int DP>
+hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st) {
+  return kv ? launch(&k_attn_bwd<T, DP, attn_nt(DP, true), kAttnWaves, true>, grid, 64 * kAttnWaves, a, st)
+            : launch(&k_attn_bwd<T, DP, attn_nt(DP, false), kAttnWaves, false>, grid, 64 * kAttnWaves, a, st);
+}
+#define GS_ATTN_INSTANCE(T, DP)                                                               \
+  template hipError_t attn_fwd<T, DP>(const AttnFwdArgs&, bool, int64_t, hipStream_t);        \
+  template hipError_t attn_bwd<T, DP>(const AttnBwdArgs&, bool, int64_t, hipStream_t);
+#if GS_PART == 1 || GS_PART == -1
+GS_ATTN_INSTANCE(F16, 64)
+#endif
+#if GS_PART == 2 || GS_PART == -1
+GS_ATTN_INSTANCE(F16, 128)
+#endif
+#if GS_PART == 3 || GS_PART == -1
+GS_ATTN_INSTANCE(F16, 256)
+#endif
+#if GS_PART == 4 || GS_PART == -1
+GS_ATTN_INSTANCE(BF16, 64)
+#endif
+#if GS_PART == 5 || GS_PART == -1
+GS_ATTN_INSTANCE(BF16, 128)
+#endif
+#if GS_PART == 6 || GS_PART == -1
+GS_ATTN_INSTANCE(BF16, 256)
+#endif
+#endif  // GS_PART != 0
+
+#if GS_PART <= 0
+
+// Clears words by a kernel: a memset node would not survive graph replays.
+__global__ void k_attn_clear(uint32_t* p) {
+  if (threadIdx.x < 2) p[threadIdx.x] = 0;
+}
+
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxStride = (int64_t)1 << 44;
+constexpr int64_t kMaxGrid = 0x7fffffff;
+
+int padded_width(int64_t D, int64_t C) {
+  const int64_t w = D > C ? D : C;
+  return w <= 64 ? 64 : w <= 128 ? 128 : 256;
+}
+
+gs_status check(const gs_attention_problem* p) {
+  if (!p) return GS_ERR_NULL_POINTER;
+  if (p->B < 0 || p->B > (1 << 20) || p->M < 0 || p->M > kMaxRows || p->N < 0 || p->N > kMaxRows ||
+      p->Hkv < 1 || p->Hq < p->Hkv || p->Hq > (1 << 14) || p->Hq % p->Hkv || p->D < 1 ||
+      p->D > GAUSS_SUM_MAX_DIM || p->C < 1 || p->C > GAUSS_SUM_MAX_DIM || p->window < 0 ||
+      p->window > kMaxRows || (p->window > 0 && !p->causal))
+    return GS_ERR_BAD_SHAPE;
+  if (p->dtype != GS_F16 && p->dtype != GS_BF16) return GS_ERR_UNSUPPORTED;
+  if (!(p->scale > -__builtin_inff()) || !(p->scale < __builtin_inff())) return GS_ERR_BAD_TAU;
+  return GS_SUCCESS;
+}
+
+AttnShape shape_of(const gs_attention_problem& p, const int32_t* q_index, const int32_t* k_index) {
+  AttnShape s;
+  s.q_index = q_index;
+  s.k_index = k_index;
+  s.B = (int32_t)p.B, s.M = (int32_t)p.M, s.N = (int32_t)p.N;
+  s.Hq = (int32_t)p.Hq, s.Hkv = (int32_t)p.Hkv, s.G = (int32_t)(p.Hq / p.Hkv);
+  s.D = (int32_t)p.D, s.C = (int32_t)p.C;
+  s.packed = p.packed != 0, s.causal = p.causal != 0, s.zero_rest = p.zero_rest;
+  s.window = (int32_t)p.window;
+  s.scale = p.scale;
+  return s;
+}
+
+// Address range [from, to) that an array's elements lie in.
+struct Span {
+  uintptr_t from = 0, to = 0;
+  bool meets(const Span& o) const { return from < o.to && o.from < to; }
+};
+
+Span span_of(const void* p, int64_t bytes) {
+  return {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)(bytes > 0 ? bytes : 0)};
+}
+
+// Checks one array (B x rows x H x width, 16-bit elements) and brings it into the
+// kernels' form.  An array without elements is not looked at.
+gs_status array_of(const gs_attention_array* x, int64_t B, int64_t rows, int64_t H, int64_t width, bool output,
+                   AttnArray& a, Span& span) {
+  a = AttnArray{nullptr, 0, 0, 0, 0};
+  span = Span{};
+  if (B == 0 || rows == 0) return GS_SUCCESS;
+  if (!x || !x->data) return GS_ERR_NULL_POINTER;
+  if (reinterpret_cast<uintptr_t>(x->data) & 1) return GS_ERR_MISALIGNED;
+  int64_t st[3] = {B > 1 ? x->batch_stride : 0, rows > 1 ? x->row_stride : 0, H > 1 ? x->head_stride : 0};
+  int64_t n[3] = {B, rows, H};
+  for (int64_t v : st)
+    if (v < 0 || v > kMaxStride) return GS_ERR_BAD_SHAPE;
+  __int128 last = width;
+  for (int i = 0; i < 3; ++i) last += (__int128)(n[i] - 1) * st[i];
+  if (last > ((__int128)1 << 60)) return GS_ERR_BAD_SHAPE;
+  a.p = static_cast<char*>(x->data);
+  a.sb = 2 * st[0], a.sr = 2 * st[1], a.sh = 2 * st[2];
+  span = span_of(x->data, 2 * (int64_t)last);
+  const int wide = output ? 4 : 8;  // elements of one access
+  a.vec = width % wide == 0 && (reinterpret_cast<uintptr_t>(x->data) & (2 * wide - 1)) == 0 &&
+          st[0] % wide == 0 && st[1] % wide == 0 && st[2] % wide == 0;
+  if (output) {  // distinct elements: dimensions by stride, each past all before it
+    int64_t extent = width;
+    for (int round = 0; round < 3; ++round) {
+      int best = -1;
+      for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (best < 0 || st[i] < st[best])) best = i;
+      if (best < 0) break;
+      if (st[best] < extent) return GS_ERR_ALIAS;
+      extent += (n[best] - 1) * st[best];
+      n[best] = 1;
+    }
+  }
+  return GS_SUCCESS;
+}
+
+// |scale| log2 e, not below the smallest normal number: masked scores are -inf, and
+// 0 * -inf is NaN (2^-126 times a score is 0 to every digit of the exponent).
+float forward_factor(float scale) {
+  const float c = (scale < 0 ? -scale : scale) * kLog2e;
+  return c > 0x1p-126f ? c : 0x1p-126f;
+}
+
+// Tiles of one head: all sequences' (packed: as many as there can be, and one for
+// the rows behind the last sequence) or one sequence's.
+int64_t tiles_of(const gs_attention_problem& p, int64_t rows, int tile) {
+  return p.packed ? rows / tile + p.B + 1 : (rows + tile - 1) / tile;
+}
+
+struct Carve {
+  char* base;
+  size_t off = 0;
+  template <typename X>
+  X* take(int64_t n) {
+    X* r = base ? reinterpret_cast<X*>(base + off) : nullptr;
+    off += ((size_t)n * sizeof(X) + 255) & ~(size_t)255;
+    return r;
+  }
+};
+
+struct BwdWork {
+  uint32_t* norms;
+  float* delta;
+  size_t total;
+};
+
+int64_t row_heads(const gs_attention_problem& p) { return (p.packed ? 1 : p.B) * p.M * p.Hq; }
+
+BwdWork bwd_work(const gs_attention_problem& p, void* ws) {
+  Carve c{static_cast<char*>(ws)};
+  BwdWork w;
+  w.norms = c.take<uint32_t>(2);
+  w.delta = c.take<float>(row_heads(p));
+  w.total = c.off;
+  return w;
+}
+
+gs_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (need == 0) return GS_SUCCESS;
+  if (!ws || have < need) return GS_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(ws) & 255) return GS_ERR_MISALIGNED;
+  return GS_SUCCESS;
+}
+
+// Any of the outputs over any of the others.
+bool overlaps(const Span* out, int outs, const Span* in, int ins) {
+  for (int i = 0; i < outs; ++i) {
+    for (int j = 0; j < ins; ++j)
+      if (out[i].meets(in[j])) return true;
+    for (int j = 0; j < i; ++j)
+      if (out[i].meets(out[j])) return true;
+  }
+  return false;
+}
+
+Span index_span(const gs_attention_problem& p, const int32_t* x) {
+  return x ? span_of(x, 4 * (p.B + (p.packed ? 1 : 0))) : Span{};
+}
+
+template <typename F>
+hipError_t by_type(const gs_attention_problem& p, F f) {
+  const int DP = padded_width(p.D, p.C);
+  if (p.dtype == GS_F16) return DP == 64 ? f(F16{}, std::integral_constant<int, 64>{})
+                              : DP == 128 ? f(F16{}, std::integral_constant<int, 128>{})
+                                          : f(F16{}, std::integral_constant<int, 256>{});
+  return DP == 64 ? f(BF16{}, std::integral_constant<int, 64>{})
+       : DP == 128 ? f(BF16{}, std::integral_constant<int, 128>{})
+                   : f(BF16{}, std::integral_constant<int, 256>{});
+}
+
+gs_status index_args(const gs_attention_problem& p, const int32_t* q_index, const int32_t* k_index) {
+  if (p.packed && p.B > 0 && (!q_index || !k_index)) return GS_ERR_NULL_POINTER;
+  if ((reinterpret_cast<uintptr_t>(q_index) | reinterpret_cast<uintptr_t>(k_index)) & 3) return GS_ERR_MISALIGNED;
+  return GS_SUCCESS;
+}
+
+gs_status run_fwd(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_array* k,
+                  const gs_attention_array* v, const int32_t* q_index, const int32_t* k_index,
+                  const gs_attention_array* out, const gs_attention_array* low, float* lse, hipStream_t stream) {
+  gs_status st = check(p);
+  if (st != GS_SUCCESS) return st;
+  if (p->B == 0 || p->M == 0) return GS_SUCCESS;
+  if ((st = index_args(*p, q_index, k_index)) != GS_SUCCESS) return st;
+  const int64_t B = p->packed ? 1 : p->B;
+  const int64_t tiles = tiles_of(*p, p->M, attn_fwd_rows(padded_width(p->D, p->C))), heads = p->Hq * B;
+  if (tiles * heads > kMaxGrid) return GS_ERR_BAD_SHAPE;
+  AttnFwdArgs a{};
+  Span in[5], o[3];
+  if ((st = array_of(q, B, p->M, p->Hq, p->D, false, a.q, in[0])) != GS_SUCCESS ||
+      (low && (st = array_of(low, B, p->M, p->Hq, p->C, true, a.low, o[2])) != GS_SUCCESS) ||
+      (st = array_of(k, B, p->N, p->Hkv, p->D, false, a.k, in[1])) != GS_SUCCESS ||
+      (st = array_of(v, B, p->N, p->Hkv, p->C, false, a.v, in[2])) != GS_SUCCESS ||
+      (st = array_of(out, B, p->M, p->Hq, p->C, true, a.out, o[0])) != GS_SUCCESS)
+    return st;
+  if (reinterpret_cast<uintptr_t>(lse) & 3) return GS_ERR_MISALIGNED;
+  if (lse) o[1] = span_of(lse, 4 * row_heads(*p));
+  in[3] = index_span(*p, q_index), in[4] = index_span(*p, k_index);
+  if (overlaps(o, 3, in, 5)) return GS_ERR_ALIAS;
+
+  a.s = shape_of(*p, q_index, k_index);
+  a.lse = lse;
+  a.lse_sb = p->packed ? 0 : p->Hq * p->M;
+  a.lse_sh = p->M;
+  a.per = 1;
+  a.tiles = (int32_t)tiles, a.heads = (int32_t)heads;
+  a.neg = p->scale < 0;
+  a.c = forward_factor(p->scale);
+  const hipError_t e = by_type(*p, [&](auto t, auto dp) {
+    return attn_fwd<decltype(t), decltype(dp)::value>(a, false, tiles * heads, stream);
+  });
+  return e == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
+}
+
+gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_array* k,
+                  const gs_attention_array* v, const int32_t* q_index, const int32_t* k_index,
+                  const gs_attention_array* out, const gs_attention_array* low, const float* lse,
+                  const gs_attention_array* dout,
+                  const gs_attention_array* dq, const gs_attention_array* dk, const gs_attention_array* dv, void* ws,
+                  size_t ws_bytes, hipStream_t stream) {
+  gs_status st = check(p);
+  if (st != GS_SUCCESS) return st;
+  if (!dq && !dk && !dv) return GS_ERR_NULL_POINTER;
+  if (p->B == 0 || (p->M == 0 && p->N == 0)) return GS_SUCCESS;
+  if ((st = index_args(*p, q_index, k_index)) != GS_SUCCESS) return st;
+  const int64_t B = p->packed ? 1 : p->B;
+  AttnBwdArgs a{};
+  AttnArray ao, alow{};
+  Span in[9], o[4];
+  if ((st = array_of(q, B, p->M, p->Hq, p->D, false, a.q, in[0])) != GS_SUCCESS ||
+      (st = array_of(k, B, p->N, p->Hkv, p->D, false, a.k, in[1])) != GS_SUCCESS ||
+      (st = array_of(v, B, p->N, p->Hkv, p->C, false, a.v, in[2])) != GS_SUCCESS ||
+      (st = array_of(out, B, p->M, p->Hq, p->C, false, ao, in[3])) != GS_SUCCESS ||
+      (low && (st = array_of(low, B, p->M, p->Hq, p->C, false, alow, in[8])) != GS_SUCCESS) ||
+      (st = array_of(dout, B, p->M, p->Hq, p->C, false, a.dout, in[4])) != GS_SUCCESS ||
+      (dq && (st = array_of(dq, B, p->M, p->Hq, p->D, true, a.dq, o[0])) != GS_SUCCESS) ||
+      (dk && (st = array_of(dk, B, p->N, p->Hkv, p->D, true, a.dk, o[1])) != GS_SUCCESS) ||
+      (dv && (st = array_of(dv, B, p->N, p->Hkv, p->C, true, a.dv, o[2])) != GS_SUCCESS))
+    return st;
+  if (p->M > 0 && !lse) return GS_ERR_NULL_POINTER;
+  if (reinterpret_cast<uintptr_t>(lse) & 3) return GS_ERR_MISALIGNED;
+  if (lse) in[5] = span_of(lse, 4 * row_heads(*p));
+  in[6] = index_span(*p, q_index), in[7] = index_span(*p, k_index);
+  const BwdWork w = bwd_work(*p, ws);
+  if ((st = check_workspace(ws, ws_bytes, w.total)) != GS_SUCCESS) return st;
+  o[3] = span_of(ws, (int64_t)w.total);
+  if (overlaps(o, 4, in, 9)) return GS_ERR_ALIAS;
+
+  const int DP = padded_width(p->D, p->C);
+  a.s = shape_of(*p, q_index, k_index);
+  a.lse = lse;
+  a.delta = w.delta;
+  a.st_sb = p->packed ? 0 : p->Hq * p->M;
+  a.st_sh = p->M;
+  a.c = p->scale * kLog2e;
+  const bool scaling = p->dtype == GS_F16;
+  a.norms = scaling ? w.norms : nullptr;
+
+  AttnPrepArgs pr{};
+  pr.s = a.s;
+  pr.out = ao, pr.low = alow, pr.dout = a.dout, pr.v = a.v;
+  pr.delta = w.delta;
+  pr.st_sb = a.st_sb, pr.st_sh = a.st_sh;
+  pr.norms = scaling ? w.norms : nullptr;
+  pr.q_units = row_heads(*p);
+  pr.k_units = scaling ? B * p->N * p->Hkv : 0;
+  const int64_t q_blocks = (pr.q_units + 15) / 16, k_blocks = (pr.k_units + 15) / 16;
+  pr.q_blocks = (int32_t)q_blocks;
+
+  const int64_t q_tiles = tiles_of(*p, p->M, attn_bwd_cols(DP, false)), q_heads = p->Hq * B;
+  const int64_t k_tiles = tiles_of(*p, p->N, attn_bwd_cols(DP, true)), k_heads = p->Hkv * B;
+  if (q_tiles * q_heads > kMaxGrid || k_tiles * k_heads > kMaxGrid || q_blocks + k_blocks > kMaxGrid)
+    return GS_ERR_BAD_SHAPE;
+
+  hipError_t e = hipSuccess;
+  if (scaling) e = launch(&k_attn_clear, 1, 64, w.norms, stream);
+  if (e != hipSuccess) return GS_ERR_HIP;
+  e = q_blocks + k_blocks == 0 ? hipSuccess
+      : p->dtype == GS_F16     ? launch(&k_attn_prep<F16>, q_blocks + k_blocks, 256, pr, stream)
+                               : launch(&k_attn_prep<BF16>, q_blocks + k_blocks, 256, pr, stream);
+  if (e != hipSuccess) return GS_ERR_HIP;
+  for (int kv = 0; kv < 2; ++kv) {
+    if (kv ? (!dk && !dv) || p->N == 0 : !dq || p->M == 0) continue;
+    a.tiles = (int32_t)(kv ? k_tiles : q_tiles);
+    a.heads = (int32_t)(kv ? k_heads : q_heads);
+    e = by_type(*p, [&](auto t, auto dp) {
+      return attn_bwd<decltype(t), decltype(dp)::value>(a, kv != 0, (int64_t)a.tiles * a.heads, stream);
+    });
+    if (e != hipSuccess) return GS_ERR_HIP;
+  }
+  return GS_SUCCESS;
+}
+
+// The pages of a cache.
+gs_status cache_of(const gs_attention_problem& p, const gs_attention_cache* c, bool output, AttnArray& k, AttnArray& v,
+                   AttnPages& pg, Span& ks, Span& vs) {
+  if (!c) return GS_ERR_NULL_POINTER;
+  if (c->pages < 0 || c->pages > kMaxRows || c->page_size < 1 || c->page_size > kMaxRows || c->table_width < 0 ||
+      c->table_width > kMaxRows || (c->table_width > 0 && c->page_size > kMaxRows / c->table_width))
+    return GS_ERR_BAD_SHAPE;
+  if (!c->lens || (c->table_width > 0 && !c->table)) return GS_ERR_NULL_POINTER;
+  if ((reinterpret_cast<uintptr_t>(c->lens) | reinterpret_cast<uintptr_t>(c->table)) & 3) return GS_ERR_MISALIGNED;
+  gs_status st = array_of(&c->k, c->pages, c->page_size, p.Hkv, p.D, output, k, ks);
+  if (st == GS_SUCCESS) st = array_of(&c->v, c->pages, c->page_size, p.Hkv, p.C, output, v, vs);
+  if (st != GS_SUCCESS) return st;
+  if (output && c->pages > 0) {  // pages are written in 16-byte pieces
+    const gs_attention_array* x[2] = {&c->k, &c->v};
+    AttnArray* y[2] = {&k, &v};
+    for (int i = 0; i < 2; ++i) {
+      AttnArray in;
+      Span s;
+      if ((st = array_of(x[i], c->pages, c->page_size, p.Hkv, i ? p.C : p.D, false, in, s)) != GS_SUCCESS) return st;
+      y[i]->vec = in.vec;
+    }
+  }
+  pg.table = c->table;
+  pg.lens = c->lens;
+  pg.page_stride_k = k.sb, pg.page_stride_v = v.sb;
+  pg.width = (int32_t)c->table_width, pg.pages = (int32_t)c->pages, pg.size = (int32_t)c->page_size;
+  pg.shift = (c->page_size & (c->page_size - 1)) ? -1 : __builtin_ctzll((unsigned long long)c->page_size);
+  return GS_SUCCESS;
+}
+
+gs_status run_paged(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_cache* cache,
+                    const int32_t* q_index, const gs_attention_array* out, float* lse, hipStream_t stream) {
+  gs_status st = check(p);
+  if (st != GS_SUCCESS) return st;
+  if (!p->causal) return GS_ERR_UNSUPPORTED;
+  if (p->B == 0 || p->M == 0) return GS_SUCCESS;
+  if (p->packed ? !q_index : q_index != nullptr) return p->packed ? GS_ERR_NULL_POINTER : GS_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(q_index) & 3) return GS_ERR_MISALIGNED;
+  const int64_t B = p->packed ? 1 : p->B, G = p->Hq / p->Hkv;
+  AttnFwdArgs a{};
+  Span in[6], o[2];
+  if ((st = array_of(q, B, p->M, p->Hq, p->D, false, a.q, in[0])) != GS_SUCCESS ||
+      (st = cache_of(*p, cache, false, a.k, a.v, a.pg, in[1], in[2])) != GS_SUCCESS ||
+      (st = array_of(out, B, p->M, p->Hq, p->C, true, a.out, o[0])) != GS_SUCCESS)
+    return st;
+  if (reinterpret_cast<uintptr_t>(lse) & 3) return GS_ERR_MISALIGNED;
+  if (lse) o[1] = span_of(lse, 4 * row_heads(*p));
+  in[3] = index_span(*p, q_index);
+  in[4] = span_of(cache->lens, 4 * p->B);
+  in[5] = span_of(cache->table, 4 * p->B * cache->table_width);
+  if (overlaps(o, 2, in, 6)) return GS_ERR_ALIAS;
+  if (p->M * G > kMaxRows) return GS_ERR_BAD_SHAPE;
+
+  a.s = shape_of(*p, q_index, nullptr);
+  a.lse = lse;
+  a.lse_sb = p->packed ? 0 : p->M;
+  a.lse_sh = p->M * B;
+  a.per = (int32_t)G;
+  const int rows = attn_fwd_rows(padded_width(p->D, p->C));
+  const int64_t tiles = tiles_of(*p, p->M * G, rows), heads = p->Hkv * B;
+  if (tiles * heads > kMaxGrid) return GS_ERR_BAD_SHAPE;
+  a.tiles = (int32_t)tiles, a.heads = (int32_t)heads;
+  a.neg = p->scale < 0;
+  a.c = forward_factor(p->scale);
+  const hipError_t e = by_type(*p, [&](auto t, auto dp) {
+    return attn_fwd<decltype(t), decltype(dp)::value>(a, true, tiles * heads, stream);
+  });
+  return e == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
+}
+
+gs_status run_append(const gs_attention_problem* p, const gs_attention_array* k, const gs_attention_array* v,
+                     const gs_attention_cache* cache, const int32_t* q_index, hipStream_t stream) {
+  gs_status st = check(p);
+  if (st != GS_SUCCESS) return st;
+  if (p->B == 0 || p->M == 0) return GS_SUCCESS;
+  if (p->packed ? !q_index : q_index != nullptr) return p->packed ? GS_ERR_NULL_POINTER : GS_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(q_index) & 3) return GS_ERR_MISALIGNED;
+  const int64_t B = p->packed ? 1 : p->B;
+  AttnAppendArgs a{};
+  Span in[5], o[2];
+  if ((st = array_of(k, B, p->M, p->Hkv, p->D, false, a.k, in[0])) != GS_SUCCESS ||
+      (st = array_of(v, B, p->M, p->Hkv, p->C, false, a.v, in[1])) != GS_SUCCESS ||
+      (st = cache_of(*p, cache, true, a.kp, a.vp, a.pg, o[0], o[1])) != GS_SUCCESS)
+    return st;
+  in[2] = index_span(*p, q_index);
+  in[3] = span_of(cache->lens, 4 * p->B);
+  in[4] = span_of(cache->table, 4 * p->B * cache->table_width);
+  if (overlaps(o, 2, in, 5)) return GS_ERR_ALIAS;
+  if (cache->table_width == 0 || cache->pages == 0) return GS_SUCCESS;
+  a.s = shape_of(*p, q_index, nullptr);
+  a.chunks = (int32_t)(((p->D > p->C ? p->D : p->C) + 7) / 8);
+  a.units = B * p->M * p->Hkv * a.chunks;
+  const int64_t grid = (a.units + 255) / 256;
+  if (grid > kMaxGrid) return GS_ERR_BAD_SHAPE;
+  return launch(&k_attn_append, grid, 256, a, stream) == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
+}
+
+}  // namespace
+#endif  // GS_PART <= 0
+}  // namespace gs
+
+#if GS_PART <= 0
+extern "C" {
+
+size_t gs_attention_fwd_workspace_size(const gs_attention_problem* p) {
+  (void)p;
+  return 0;
+}
+
+gs_status gs_attention_fwd(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_array* k,
+                           const gs_attention_array* v, const int32_t* q_index, const int32_t* k_index,
+                           const gs_attention_array* out, const gs_attention_array* low, float* lse,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  (void)workspace, (void)workspace_bytes;
+  return gs::run_fwd(p, q, k, v, q_index, k_index, out, low, lse, stream);
+}
+
+size_t gs_attention_bwd_workspace_size(const gs_attention_problem* p, int want_dq, int want_dk, int want_dv) {
+  if (gs::check(p) != GS_SUCCESS || (!want_dq && !want_dk && !want_dv)) return 0;
+  return gs::bwd_work(*p, nullptr).total;
+}
+
+gs_status gs_attention_bwd(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_array* k,
+                           const gs_attention_array* v, const int32_t* q_index, const int32_t* k_index,
+                           const gs_attention_array* out, const gs_attention_array* low, const float* lse,
+                  const gs_attention_array* dout,
+                           const gs_attention_array* dq, const gs_attention_array* dk, const gs_attention_array* dv,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return gs::run_bwd(p, q, k, v, q_index, k_index, out, low, lse, dout, dq, dk, dv, workspace, workspace_bytes, stream);
+}
+
+size_t gs_attention_paged_workspace_size(const gs_attention_problem* p, const gs_attention_cache* cache) {
+  (void)p, (void)cache;
+  return 0;
+}
+
+gs_status gs_attention_paged(const gs_attention_problem* p, const gs_attention_array* q,
+                             const gs_attention_cache* cache, const int32_t* q_index, const gs_attention_array* out,
+                             float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  (void)workspace, (void)workspace_bytes;
+  return gs::run_paged(p, q, cache, q_index, out, lse, stream);
+}
+
+gs_status gs_attention_append(const gs_attention_problem* p, const gs_attention_array* k,
+                              const gs_attention_array* v, const gs_attention_cache* cache, const int32_t* q_index,
+                              hipStream_t stream) {
+  return gs::run_append(p, k, v, cache, q_index, stream);
+}
+
+}  // extern "C"
+#endif  // GS_PART <= 0

@@ -1,0 +1,361 @@
+// gs_attn.h -- operand layouts and helpers shared by the softmax-attention
+// kernels (gfx950 / CDNA4).
+//
+// As in the Gauss-sum kernels every contraction runs on the 16x16x32 matrix
+// instruction in the transposed orientation: the rows of a streamed tile stand
+// on the MFMA row index, the wave's own ("column") points on the lane index, so
+// a lane holds 4 of the 16 rows of one column and the packed result of two row
+// tiles is the B operand of the next contraction over those rows:
+//     A operand: A[i = l%16][k = 8*(l/16) .. +7]
+//     B operand: B[k = 8*(l/16) .. +7][j = l%16]
+//     result   : D[i = 4*(l/16) + r][j = l%16]
+// The contraction over 32 rows takes slot k = 8 g + z of lane group g = l/16 to
+// row 16 (z / 4) + 4 g + z % 4, for which two transposing LDS reads give the
+// A operand straight from the row-major tile.
+//
+// Tiles are copied from the caller's arrays to LDS without a register round trip
+// (16 bytes a lane) where rows are 16-byte aligned and a multiple of 8 wide, and
+// element by element otherwise.  A tile row is DP 16-bit elements (DP = 64, 128
+// or 256, columns past the caller's width zero); its 16-byte chunk c lies at
+// chunk c ^ swz(row), so the row reads (eight rows, one chunk) and the
+// transposing reads (four rows, two chunks) both spread over the banks.
+#pragma once
+
+#include "gs_common.h"
+
+namespace gs {
+
+constexpr int kNoRow = -1;
+constexpr int kRestOut = 1, kRestLse = 2;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// One array of the caller: element (sequence b, row i, head h, column) at
+// p + b*sb + i*sr + h*sh + 2*column (bytes; 4*column for 32-bit data).
+struct AttnArray {
+  char* p;
+  int64_t sb, sr, sh;
+  int32_t vec;  // rows 16-byte aligned and a multiple of 8 elements wide
+};
+
+// What every kernel of a call knows of it.
+struct AttnShape {
+  const int32_t* q_index;  // packed: B + 1 offsets; dense: B lengths or NULL
+  const int32_t* k_index;
+  int32_t B, M, N;         // dense: rows / keys of a sequence; packed: of all sequences together
+  int32_t Hq, Hkv, G;      // G = Hq / Hkv
+  int32_t D, C;
+  int32_t packed, causal;
+  int32_t zero_rest;       // rows of no sequence: kRestOut, kRestLse
+  int32_t window;          // 0: none
+  float scale;             // of the scores (natural units)
+};
+
+// One sequence: first row and count of its queries and keys.
+struct AttnSeq {
+  int32_t q0, qn, k0, kn;
+};
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// First row and length of sequence b on one side (lengths and offsets are read
+// as they are and brought into range, so no index leaves the arrays).
+__device__ __forceinline__ void seq_side(const int32_t* index, int packed, int b, int rows, int& first, int& n) {
+  if (packed) {
+    first = clampi(index[b], 0, rows);
+    n = clampi(index[b + 1], first, rows) - first;
+  } else {
+    first = 0;
+    n = index ? clampi(index[b], 0, rows) : rows;
+  }
+}
+
+__device__ __forceinline__ AttnSeq seq_of(const AttnShape& s, int b) {
+  AttnSeq r;
+  seq_side(s.q_index, s.packed, b, s.M, r.q0, r.qn);
+  seq_side(s.k_index, s.packed, b, s.N, r.k0, r.kn);
+  return r;
+}
+
+// Tile `slot` of the packed rows: its sequence and its index within it.  The
+// tiles of all sequences (ceil(n * per / tile) each) are counted by one wave scan
+// of the offsets, 64 sequences a step.  Returns kNoRow where there is none, t then
+// being the number of tiles.
+__device__ __forceinline__ int packed_tile(const int32_t* off, int B, int rows, int per, int tile, int slot,
+                                           int& t) {
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    int n = 0;
+    if (b0 + lane < B) {
+      const int e0 = clampi(off[b0 + lane], 0, rows);
+      n = clampi(off[b0 + lane + 1], e0, rows) - e0;
+      n = (int)(((int64_t)n * per + tile - 1) / tile);
+    }
+    int end = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int x = __shfl_up(end, d);
+      if (lane >= d) end += x;
+    }
+    const uint64_t hit = __ballot(slot - base < end);
+    if (hit) {
+      const int w = __builtin_ctzll(hit);
+      t = slot - base - __builtin_amdgcn_readlane(end - n, w);
+      return b0 + w;
+    }
+    base += __builtin_amdgcn_readlane(end, 63);
+  }
+  t = base;
+  return kNoRow;
+}
+
+// Streams and tiles of a launch: block id -> (tile, head).  Blocks go to the
+// eight XCDs in turn, and each XCD has an L2 of its own: with a multiple of eight
+// (sequence, head) streams every XCD gets a contiguous run of them, so the query
+// heads that share a key head read its keys through one L2.
+__device__ __forceinline__ void block_place(int id, int heads, int& tile, int& head) {
+  tile = id / heads;
+  const int p = id - tile * heads;
+  head = (heads & 7) == 0 ? (p & 7) * (heads >> 3) + (p >> 3) : p;
+}
+
+// Rows that column point `at` (its index in its sequence) sees on the other
+// side: [lo, hi).  ahead = keys - queries.  Queries see keys up to their own
+// place (causal) and the last `window` of them; keys are seen the other way
+// round.
+__device__ __forceinline__ void query_range(const AttnShape& s, int at, int ahead, int kn, int& lo, int& hi) {
+  lo = 0, hi = kn;
+  if (s.causal) {
+    const int end = at + ahead + 1;  // may be negative: nothing seen
+    hi = clampi(end, 0, kn);
+    if (s.window > 0 && end > s.window) lo = end - s.window;  // lo <= end, and hi = min(end, kn)
+    lo = lo > hi ? hi : lo;
+  }
+}
+__device__ __forceinline__ void key_range(const AttnShape& s, int at, int ahead, int qn, int& lo, int& hi) {
+  lo = 0, hi = qn;
+  if (s.causal) {
+    const int64_t first = (int64_t)at - ahead;
+    lo = first < 0 ? 0 : first > qn ? qn : (int)first;
+    if (s.window > 0) {
+      const int64_t end = first + s.window;
+      hi = end < lo ? lo : end < qn ? (int)end : qn;
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<F16>(float lo, float hi) {
+  return pack_f16(lo, hi);
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+template <>
+__device__ __forceinline__ uint32_t pack2<BF16>(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{lo, hi}, bf16x2));
+}
+
+template <typename T>
+constexpr uint32_t exponent_bits() {
+  return sizeof(typename T::storage) == 2 && __is_same(T, F16) ? 0x7c00u : 0x7f80u;
+}
+
+// Whether any of the eight elements is an infinity or NaN.
+template <typename T>
+__device__ __forceinline__ bool not_finite(const uint4& a) {
+  constexpr uint32_t e = exponent_bits<T>();
+  bool bad = false;
+  for (uint32_t x : {a.x, a.y, a.z, a.w}) bad |= (x & e) == e || ((x >> 16) & e) == e;
+  return bad;
+}
+
+// ------------------------------------------------------------------ LDS tiles
+
+typedef __attribute__((address_space(3))) char attn_lds;
+__device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(const attn_lds*)p; }
+
+// 64 lanes x 16 bytes from per-lane addresses to LDS bytes m0 + 16 * lane.
+// Assembly, so that the compiler neither sees nor waits for the copy: the
+// tile loop waits (copies_done) before the barrier that publishes it.  The
+// s_nop separates the write of m0 from its use.
+__device__ __forceinline__ void copy16(const char* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(lds), "v"(src)
+               : "memory", "m0");
+}
+
+// Every copy and LDS access of this wave done, then the workgroup's barrier.
+__device__ __forceinline__ void tile_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+__host__ __device__ constexpr int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+
+constexpr uint32_t kNanPair = 0x7fff7fffu;  // NaN in fp16 and in bf16
+
+// ROWS rows of DP elements into LDS by THREADS threads.  row(r) gives the address
+// of tile row r (never past the caller's array), or NULL for a row that is read
+// as NaN.
+template <int DP, int ROWS, int THREADS, typename Row>
+__device__ __forceinline__ void load_tile(char* tile, int width, int vec, Row row) {
+  constexpr int NCH = DP / 8;
+  static_assert(ROWS * NCH % THREADS == 0, "whole waves");
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+#pragma unroll
+  for (int it = 0; it < ROWS * NCH / THREADS; ++it) {
+    const int at = it * THREADS + tid;
+    const int r = at / NCH, c = (at % NCH) ^ swz(r);
+    const char* src = row(r);
+    if (vec) {
+      if (c * 8 < width) {
+        if (src)
+          copy16(src + c * 16, __builtin_amdgcn_readfirstlane(lds_offset(tile)) + (it * THREADS + wave * 64) * 16);
+        else
+          *reinterpret_cast<uint4*>(tile + at * 16) = uint4{kNanPair, kNanPair, kNanPair, kNanPair};
+      }
+    } else {
+      uint32_t x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        x[e] = c * 8 + e >= width ? 0u : src ? reinterpret_cast<const uint16_t*>(src)[c * 8 + e] : 0x7fffu;
+      *reinterpret_cast<uint4*>(tile + at * 16) =
+          uint4{x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
+    }
+  }
+}
+
+// Zeros over all of a workgroup's tiles: the columns past the caller's width are
+// not written by the copies.
+template <int THREADS>
+__device__ __forceinline__ void clear_tiles(char* tiles, int bytes) {
+  for (int at = threadIdx.x * 16; at < bytes; at += THREADS * 16)
+    *reinterpret_cast<uint4*>(tiles + at) = uint4{0, 0, 0, 0};
+}
+
+// The lane's places in a tile: row operands (row l%16, chunk 4c + l/16) and
+// transposed operands (rows 4 (l/16) .. +3, columns 16 ct + 4 (l%4) .. +3).
+template <int DP>
+struct TileLane {
+  int row[2];
+  int tr[4];
+  __device__ __forceinline__ TileLane() {
+    const int l = threadIdx.x & 63, i = l & 15, g = l >> 4;
+    for (int p = 0; p < 2; ++p) row[p] = i * DP * 2 + ((4 * p + g) ^ swz(i)) * 16;
+    const int r = 4 * g + ((l >> 2) & 3);
+    for (int p = 0; p < 4; ++p) tr[p] = r * DP * 2 + ((2 * p + ((l >> 1) & 1)) ^ swz(r)) * 16 + (l & 1) * 8;
+  }
+};
+
+// Row operand: rows 16 t .. of the tile, columns 32 c .. .
+template <int DP>
+__device__ __forceinline__ uint4 row_operand(const char* tile, const TileLane<DP>& ln, int t, int c) {
+  return *reinterpret_cast<const uint4*>(tile + ln.row[c & 1] + (c >> 1) * 128 + t * 16 * DP * 2);
+}
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v lds_short4v;
+__device__ __forceinline__ uint2 read_tr(const char* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v*)(attn_lds*)p));
+}
+// Transposed operand: columns 16 ct .. of the tile on the MFMA rows, its rows
+// 32 s .. +31 contracted.
+template <int DP>
+__device__ __forceinline__ uint4 tr_operand(const char* tile, const TileLane<DP>& ln, int s, int ct) {
+  const char* p = tile + ln.tr[ct & 3] + (ct >> 2) * 128 + s * 32 * DP * 2;
+  const uint2 a = read_tr(p), b = read_tr(p + 16 * DP * 2);
+  return uint4{a.x, a.y, b.x, b.y};
+}
+
+// f applied to the eight 16-bit elements.
+template <typename F>
+__device__ __forceinline__ uint4 each16(const uint4& a, F f) {
+  auto two = [&](uint32_t x) { return f(x & 0xffffu) | f(x >> 16) << 16; };
+  return uint4{two(a.x), two(a.y), two(a.z), two(a.w)};
+}
+
+// acc[ct][n] += X^T B[n] over the 32 rows of step s of a tile: NC transposed
+// operands, NT column tiles.  Where some columns do not see some rows (masked)
+// B is zero there, but a row with an infinity or NaN may reach only the columns
+// that see it, and 0 * NaN is NaN.  Such elements are then contracted apart:
+// the rest of the operand as it is, and the products' infinities by their signs, as
+// counts of +inf and -inf (an element that is NaN counts as both, and
+// inf - inf is NaN again).
+template <typename T, int DP, bool SIGNED, int NC, int NT>
+__device__ __forceinline__ void contract(const char* tile, const TileLane<DP>& ln, int s, const uint4 (&b)[NT],
+                                         floatx4 (&acc)[NC][NT], bool masked) {
+  constexpr uint32_t e = exponent_bits<T>(), one = __is_same(T, F16) ? 0x3c00u : 0x3f80u;
+  bool apart = false;
+  if (masked) {
+    bool bad = false;
+#pragma unroll
+    for (int ct = 0; ct < NC; ++ct) bad |= not_finite<T>(tr_operand<DP>(tile, ln, s, ct));
+    apart = __any(bad);
+  }
+#pragma unroll
+  for (int ct = 0; ct < NC; ++ct) {
+    uint4 a = tr_operand<DP>(tile, ln, s, ct);
+    if (apart) {
+      const uint4 up = each16(a, [=](uint32_t x) { return (x & e) == e && (x != (e | 0x8000u)) ? one : 0u; });
+      const uint4 down = each16(a, [=](uint32_t x) { return (x & e) == e && x != e ? one : 0u; });
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint4 bp = each16(b[n], [=](uint32_t x) { return x != 0 && x < 0x8000u ? one : 0u; });
+        floatx4 inf = mfma_qk<T>(up, bp, floatx4{0, 0, 0, 0}), ninf = mfma_qk<T>(down, bp, floatx4{0, 0, 0, 0});
+        if (SIGNED) {
+          const uint4 bn = each16(b[n], [=](uint32_t x) { return x > 0x8000u ? one : 0u; });
+          inf = mfma_qk<T>(down, bn, inf);
+          ninf = mfma_qk<T>(up, bn, ninf);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          acc[ct][n][r] += inf[r] > 0.0f ? __builtin_inff() : 0.0f;
+          acc[ct][n][r] -= ninf[r] > 0.0f ? __builtin_inff() : 0.0f;
+        }
+      }
+      a = each16(a, [=](uint32_t x) { return (x & e) == e ? 0u : x; });
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[ct][n] = mfma_qk<T>(a, b[n], acc[ct][n]);
+  }
+}
+
+// ------------------------------------------------------------- 16-bit output
+
+// Four neighbouring columns of one row, rounded to T once.
+template <typename T>
+__device__ __forceinline__ void store4(char* row, int c, int width, int vec, float x0, float x1, float x2,
+                                       float x3) {
+  const uint32_t a = pack2<T>(x0, x1), b = pack2<T>(x2, x3);
+  uint16_t* p = reinterpret_cast<uint16_t*>(row) + c;
+  if (vec) {
+    if (c < width) *reinterpret_cast<uint2*>(p) = uint2{a, b};
+  } else {
+    if (c < width) p[0] = (uint16_t)a;
+    if (c + 1 < width) p[1] = (uint16_t)(a >> 16);
+    if (c + 2 < width) p[2] = (uint16_t)b;
+    if (c + 3 < width) p[3] = (uint16_t)(b >> 16);
+  }
+}
+
+// What rounding x to T leaves.
+template <typename T>
+__device__ __forceinline__ float left(float x) {
+  return x - T::to_float((uint16_t)pack2<T>(x, 0.0f));
+}
+
+// Zeros in rows first + part, first + part + parts, ... < rows of one head.
+__device__ __forceinline__ void zero_rows(const AttnArray& x, int b, int head, int width, int first, int rows,
+                                          int part, int parts) {
+  for (int64_t r = first + part; r < rows; r += parts) {
+    uint16_t* p = reinterpret_cast<uint16_t*>(x.p + b * x.sb + r * x.sr + head * x.sh);
+    for (int c = threadIdx.x; c < width; c += blockDim.x) p[c] = 0;
+  }
+}
+
+}  // namespace gs

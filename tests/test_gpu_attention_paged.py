@@ -1,0 +1,241 @@
+"""Attention over a paged cache on the GPU against 64 bits: chunks and single tokens, pages that
+end inside a tile, long caches, bad page numbers, and a decode loop against dense attention."""
+import math
+
+import pytest
+import torch
+
+import attention_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def at():
+    from paper_2609_04910_amd import attention
+    attention.load()
+    return attention
+
+
+def normal(gen, shape, dtype, std=1.0):
+    return (torch.randn(shape, generator=gen, dtype=torch.float64) * std).to(dtype).cuda()
+
+
+def offsets(lens):
+    return torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device="cuda")
+
+
+class Cache:
+    """Pages in shuffled order with unused ones that hold NaN, and a table wider than needed."""
+
+    def __init__(self, gen, lens, page, Hkv, D, C, dtype, spare=3):
+        used = [-(-n // page) for n in lens]
+        total = sum(used) + spare
+        order = torch.randperm(total, generator=gen).tolist()
+        self.k = torch.full((total, page, Hkv, D), math.nan, dtype=dtype, device="cuda")
+        self.v = torch.full((total, page, Hkv, C), math.nan, dtype=dtype, device="cuda")
+        self.keys = [(normal(gen, (n, Hkv, D), dtype), normal(gen, (n, Hkv, C), dtype)) for n in lens]
+        table = torch.full((len(lens), max(used + [0]) + 2), -1, dtype=torch.int32)
+        self.pages = []
+        for b, n in enumerate(lens):
+            mine = [order.pop() for _ in range(used[b])]
+            self.pages.append(mine)
+            table[b, :used[b]] = torch.tensor(mine, dtype=torch.int32)
+            for i, x in enumerate(mine):
+                part = slice(i * page, min(n, (i + 1) * page))
+                self.k[x, :part.stop - part.start] = self.keys[b][0][part]
+                self.v[x, :part.stop - part.start] = self.keys[b][1][part]
+        self.table = table.cuda()
+        self.lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+
+CASES = [  # new tokens, keys, page, Hq, Hkv, D, C, window
+    ([1], [1], 16, 1, 1, 64, 64, 0),
+    ([1, 1, 1], [5, 64, 200], 16, 8, 2, 128, 128, 0),
+    ([1] * 5, [1, 17, 700, 1500, 33], 20, 8, 1, 64, 64, 0),
+    ([1, 1], [900, 130], 1, 4, 4, 64, 64, 100),
+    ([1, 1], [3000, 2], 64, 16, 1, 128, 64, 0),
+    ([1, 1], [300, 70], 16, 4, 2, 256, 256, 0),
+    ([1, 1], [300, 70], 16, 4, 2, 33, 17, 0),
+    ([1, 1], [300, 70], 16, 40, 1, 80, 80, 0),
+    ([1], [9000], 16, 4, 4, 64, 64, 0),
+    ([7, 1, 0, 30], [90, 40, 12, 30], 16, 4, 2, 64, 64, 0),
+    ([130, 3], [130, 500], 32, 4, 1, 128, 128, 0),
+    ([64, 65, 200], [300, 65, 1000], 48, 6, 2, 96, 80, 150),
+    ([40, 9], [200, 64], 100, 2, 1, 256, 200, 0),
+    ([5, 0], [3, 0], 16, 2, 1, 64, 64, 0),   # more new tokens than keys: rows that see nothing
+    ([2] * 100, [40] * 100, 16, 2, 1, 64, 64, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "%d-%d-%d-%dx%d-%d" % (len(c[0]), sum(c[0]), c[2], c[3], c[4], c[5]))
+def test_against_64_bits(at, case, dtype):
+    rows, keys, page, Hq, Hkv, D, C, window = case
+    gen = torch.Generator().manual_seed(sum(keys))
+    cache = Cache(gen, keys, page, Hkv, D, C, dtype)
+    q = normal(gen, (sum(rows), Hq, D), dtype)
+    offs = offsets(rows)
+    out, lse = at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens, q_offsets=offs, window=window,
+                                  return_lse=True)
+    for b in range(len(rows)):
+        i = slice(sum(rows[:b]), sum(rows[:b + 1]))
+        r = ref.one(q[i], *cache.keys[b], D ** -0.5, True, window)
+        ref.check("out of sequence %d" % b, out[i], *r["out"])
+        ref.check("lse of sequence %d" % b, lse[:, i], *r["lse"])
+    if len(set(rows)) == 1:
+        alike, lse2 = at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens, window=window, return_lse=True)
+        for b in range(len(rows)):
+            i = slice(sum(rows[:b]), sum(rows[:b + 1]))
+            r = ref.one(q[i], *cache.keys[b], D ** -0.5, True, window)
+            ref.check("out of sequence %d" % b, alike[i], *r["out"])
+            ref.check("lse of sequence %d" % b, lse2[:, i], *r["lse"])
+
+
+def test_rows_of_no_sequence(at):
+    gen = torch.Generator().manual_seed(1)
+    cache = Cache(gen, [40, 50], 16, 1, 64, 64, torch.bfloat16)
+    q = normal(gen, (9, 2, 64), torch.bfloat16)
+    offs = torch.tensor([0, 2, 5], dtype=torch.int32, device="cuda")
+    args = (q, cache.k, cache.v, cache.table, cache.lens, offs)
+    out, lse = at.attention_paged(*args, return_lse=True)
+    assert not out[5:].any() and (lse[:, 5:] == -math.inf).all() and out[:5].isfinite().all()
+    mine = torch.full_like(out, 7.0)
+    at.attention_paged(*args, out=mine)
+    assert (mine[5:] == 7).all() and torch.equal(mine[:5], out[:5])
+
+
+@pytest.mark.parametrize("number", [-1, -2 ** 31, 1000, 2 ** 31 - 1])
+@pytest.mark.parametrize("rows", [1, 20])
+def test_bad_page_numbers(at, rows, number):
+    """A page number outside the cache: rows that see its keys are NaN, others are as they were, and
+    nothing is written there."""
+    gen = torch.Generator().manual_seed(2)
+    cache = Cache(gen, [100, 100], 16, 1, 64, 64, torch.bfloat16)
+    q = normal(gen, (2 * rows, 2, 64), torch.bfloat16)
+    good = at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens)
+    cache.table[1, 5] = number                 # keys 80 .. 95 of the second sequence
+    bad = at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens)
+    seen = torch.zeros(2 * rows, dtype=torch.bool, device="cuda")
+    seen[rows:] = torch.arange(100 - rows, 100, device="cuda") >= 80
+    assert bad[seen].isnan().all() and torch.equal(bad[~seen], good[~seen])
+    hidden = at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens, window=4)[2 * rows - 1]
+    assert hidden.isfinite().all()             # keys 96 .. 99
+    k0, v0 = cache.k.clone(), cache.v.clone()
+    k, v = normal(gen, (40, 1, 64), torch.bfloat16), normal(gen, (40, 1, 64), torch.bfloat16)
+    at.attention_append(k, v, cache.k, cache.v, cache.table, cache.lens)   # positions 80 .. 99 of both
+    changed = (cache.k.view(torch.int16) != k0.view(torch.int16)).flatten(1).any(1).nonzero().flatten().tolist()
+    assert set(changed) == {cache.pages[0][5], cache.pages[0][6], cache.pages[1][6]}
+
+
+def test_lengths_past_the_table(at):
+    """More keys than the table holds: the sequence ends with the table."""
+    gen = torch.Generator().manual_seed(3)
+    cache = Cache(gen, [64], 16, 1, 64, 64, torch.bfloat16)
+    cache.table = cache.table[:, :4].contiguous()
+    q = normal(gen, (1, 2, 64), torch.bfloat16)
+    want = at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens)
+    for n in (65, 2 ** 31 - 1):
+        cache.lens.fill_(n)
+        assert torch.equal(at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens), want)
+    cache.lens.fill_(-5)
+    assert not at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens).any()
+
+
+def test_page_offsets_past_32_bits(at):
+    """Pages more than 4 GiB into the cache."""
+    page, D, Hkv = 64, 128, 8
+    pages = (1 << 32) // (page * D * Hkv * 2) + 40
+    k = torch.zeros((pages, page, Hkv, D), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    gen = torch.Generator().manual_seed(4)
+    table = torch.tensor([[pages - 1, 3, pages - 7]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([150], dtype=torch.int32, device="cuda")
+    kn, vn = normal(gen, (150, Hkv, D), torch.bfloat16), normal(gen, (150, Hkv, D), torch.bfloat16)
+    at.attention_append(kn, vn, k, v, table, lens)
+    assert torch.equal(k[pages - 1], kn[:64]) and torch.equal(v[pages - 7, :22], vn[128:])
+    for rows in (1, 50):
+        q = normal(gen, (rows, 8, D), torch.bfloat16)
+        out = at.attention_paged(q, k, v, table, lens)
+        ref.check("out", out, *ref.one(q, kn, vn, D ** -0.5, True)["out"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,keys,page,Hkv,D,C", [([3, 0, 20], [3, 7, 50], 16, 2, 64, 64), ([1, 1, 1], [1, 16, 17], 16, 4, 128, 48),
+                                                    ([5, 2], [100, 9], 7, 1, 33, 5), ([4], [2], 16, 1, 64, 64)])
+def test_append(at, rows, keys, page, Hkv, D, C, dtype):
+    gen = torch.Generator().manual_seed(sum(keys) + D)
+    cache = Cache(gen, keys, page, Hkv, D, C, dtype)
+    k, v = normal(gen, (sum(rows) + 2, Hkv, D), dtype), normal(gen, (sum(rows) + 2, Hkv, C), dtype)
+    want = [cache.k.clone(), cache.v.clone()]
+    for b, n in enumerate(rows):
+        for i in range(n):
+            at_ = keys[b] - n + i
+            if at_ >= 0:
+                x = cache.pages[b][at_ // page]
+                want[0][x, at_ % page], want[1][x, at_ % page] = k[sum(rows[:b]) + i], v[sum(rows[:b]) + i]
+    at.attention_append(k, v, cache.k, cache.v, cache.table, cache.lens, q_offsets=offsets(rows))
+    for a, b in zip((cache.k, cache.v), want):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_prefill_and_decode_against_dense(at):
+    """Tokens appended chunk by chunk, then one by one, each time attended over the cache: the rows of
+    dense causal attention over the whole sequence."""
+    gen = torch.Generator().manual_seed(5)
+    Hq, Hkv, D, page, steps = 8, 2, 64, 16, [70, 1, 45, 1, 1, 30, 1]
+    total = [sum(steps), sum(steps) + 37]                      # the second sequence is ahead by a prompt
+    q = [normal(gen, (n, Hq, D), torch.bfloat16) for n in total]
+    k = [normal(gen, (n, Hkv, D), torch.bfloat16) for n in total]
+    v = [normal(gen, (n, Hkv, D), torch.bfloat16) for n in total]
+    want = [at.attention_fwd(q[b][None], k[b][None], v[b][None], causal=True)[0][0] for b in range(2)]
+    width = -(-max(total) // page)
+    table = torch.randperm(2 * width, generator=gen).to(torch.int32).view(2, width).cuda()
+    kp = torch.full((2 * width, page, Hkv, D), math.nan, dtype=torch.bfloat16, device="cuda")
+    vp = torch.full_like(kp, math.nan)
+    done = [0, 0]
+    lens = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for i, n in enumerate(steps):
+        new = [n, n + (37 if i == 0 else 0)]
+        lens += torch.tensor(new, dtype=torch.int32, device="cuda")
+        part = [slice(done[b], done[b] + new[b]) for b in range(2)]
+        rows = [torch.cat([x[b][part[b]] for b in range(2)]) for x in (q, k, v)]
+        offs = None if new == [1, 1] else offsets(new)
+        at.attention_append(rows[1], rows[2], kp, vp, table, lens, q_offsets=offs)
+        out = at.attention_paged(rows[0], kp, vp, table, lens, q_offsets=offs)
+        first = 0
+        for b in range(2):
+            # both are within their rounding (2 u of |out|, u of sum p |v|) of the exact rows
+            torch.testing.assert_close(out[first:first + new[b]].float(), want[b][part[b]].float(), rtol=2 ** -6, atol=2 ** -6)
+            first += new[b]
+            done[b] += new[b]
+
+
+def test_captured_decode_replays(at):
+    """A decode step (append, attend) captured once and replayed as the lengths grow in place."""
+    gen = torch.Generator().manual_seed(6)
+    cache = Cache(gen, [300, 90, 17], 16, 2, 128, 128, torch.float16)
+    cache.table = torch.arange(3 * 24, dtype=torch.int32, device="cuda").view(3, 24)
+    cache.k = normal(gen, (72, 16, 2, 128), torch.float16)
+    cache.v = normal(gen, (72, 16, 2, 128), torch.float16)
+    q, k, v = (normal(gen, (3, h, 128), torch.float16) for h in (8, 2, 2))
+
+    def step():
+        at.attention_append(k, v, cache.k, cache.v, cache.table, cache.lens)
+        return at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(4):
+        cache.lens += 1 if i else 20
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, device="cuda"))
+        held.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = held.clone()
+        assert torch.equal(got, step())
+        torch.cuda.synchronize()
