@@ -6,6 +6,7 @@
 // 1 .. GS_PARTS one dtype and padded width each.
 #include "gs_attention.h"
 
+#include <algorithm>
 #include <type_traits>
 
 #include "gs_attn_bwd.h"
@@ -21,11 +22,18 @@
 
 namespace gs {
 
-// Rows of a workgroup's waves: NQ query tiles of 16 a wave (NT column tiles in the
-// backward passes).
+// Query tiles of 16 rows a wave owns (column tiles in the backward passes), per
+// padded width: as many as its registers hold beside the operands in flight,
+// since each operand read from LDS then feeds more matrix instructions (two
+// waves a SIMD, 256 registers).  Forward of 8192 tokens, 32 heads, D = 128,
+// causal: two tiles 617 us, three 572 us, four 2750 us (spilled); D = 256
+// (2 x 2048 tokens, 8 heads): one 91 us, two 332 us (spilled).  dQ at D = 128: two
+// 807 us, three 1947 us.  dK and dV at D = 128: one 1360 us, two 3574 us, or
+// 1567 us with 512 registers and one wave a SIMD.  Eight waves a workgroup instead
+// of four: 4 to 10 % slower at every width.
 constexpr int kAttnWaves = 4;
-constexpr int attn_nq(int DP) { return 2; }
-constexpr int attn_nt(int DP, bool KV) { return DP == 256 ? 1 : 2; }
+constexpr int attn_nq(int DP) { return DP == 256 ? 1 : DP == 128 ? 3 : 2; }
+constexpr int attn_nt(int DP, bool KV) { return DP == 256 || (KV && DP == 128) ? 1 : 2; }
 
 constexpr int attn_fwd_rows(int DP) { return 16 * kAttnWaves * attn_nq(DP); }
 constexpr int attn_bwd_cols(int DP, bool KV) { return 16 * kAttnWaves * attn_nt(DP, KV); }
@@ -44,13 +52,21 @@ hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st)
 #if GS_PART != 0
 template <typename T, int DP>
 hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int64_t grid, hipStream_t st) {
-  return paged ? launch(&k_attn_fwd<T, DP, attn_nq(DP), kAttnWaves, true>, grid, 64 * kAttnWaves, a, st)
-               : launch(&k_attn_fwd<T, DP, attn_nq(DP), kAttnWaves, false>, grid, 64 * kAttnWaves, a, st);
+  constexpr int NQ = attn_nq(DP), NW = kAttnWaves;
+  const bool wide = a.k.vec && a.v.vec;
+  return launch(paged ? wide ? &k_attn_fwd<T, DP, NQ, NW, true, true> : &k_attn_fwd<T, DP, NQ, NW, true, false>
+                : wide ? &k_attn_fwd<T, DP, NQ, NW, false, true>
+                       : &k_attn_fwd<T, DP, NQ, NW, false, false>,
+                grid, 64 * NW, a, st);
 }
 template <typename T, int DP>
 hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st) {
-  return kv ? launch(&k_attn_bwd<T, DP, attn_nt(DP, true), kAttnWaves, true>, grid, 64 * kAttnWaves, a, st)
-            : launch(&k_attn_bwd<T, DP, attn_nt(DP, false), kAttnWaves, false>, grid, 64 * kAttnWaves, a, st);
+  constexpr int NQ = attn_nt(DP, false), NK = attn_nt(DP, true), NW = kAttnWaves;
+  const bool wide = kv ? a.q.vec && a.dout.vec : a.k.vec && a.v.vec;
+  return launch(kv ? wide ? &k_attn_bwd<T, DP, NK, NW, true, true> : &k_attn_bwd<T, DP, NK, NW, true, false>
+                : wide ? &k_attn_bwd<T, DP, NQ, NW, false, true>
+                       : &k_attn_bwd<T, DP, NQ, NW, false, false>,
+                grid, 64 * NW, a, st);
 }
 #define GS_ATTN_INSTANCE(T, DP)                                                               \
   template hipError_t attn_fwd<T, DP>(const AttnFwdArgs&, bool, int64_t, hipStream_t);        \
@@ -76,11 +92,6 @@ GS_ATTN_INSTANCE(BF16, 256)
 #endif  // GS_PART != 0
 
 #if GS_PART <= 0
-
-// Clears words by a kernel: a memset node would not survive graph replays.
-__global__ void k_attn_clear(uint32_t* p) {
-  if (threadIdx.x < 2) p[threadIdx.x] = 0;
-}
 
 namespace {
 
@@ -148,7 +159,7 @@ gs_status array_of(const gs_attention_array* x, int64_t B, int64_t rows, int64_t
   a.sb = 2 * st[0], a.sr = 2 * st[1], a.sh = 2 * st[2];
   span = span_of(x->data, 2 * (int64_t)last);
   const int wide = output ? 4 : 8;  // elements of one access
-  a.vec = width % wide == 0 && (reinterpret_cast<uintptr_t>(x->data) & (2 * wide - 1)) == 0 &&
+  a.vec = a.sr < (1 << 24) && width % wide == 0 && (reinterpret_cast<uintptr_t>(x->data) & (2 * wide - 1)) == 0 &&
           st[0] % wide == 0 && st[1] % wide == 0 && st[2] % wide == 0;
   if (output) {  // distinct elements: dimensions by stride, each past all before it
     int64_t extent = width;
@@ -190,8 +201,7 @@ struct Carve {
 };
 
 struct BwdWork {
-  uint32_t* norms;
-  float* delta;
+  float *norms, *delta, *lse2;
   size_t total;
 };
 
@@ -200,8 +210,9 @@ int64_t row_heads(const gs_attention_problem& p) { return (p.packed ? 1 : p.B) *
 BwdWork bwd_work(const gs_attention_problem& p, void* ws) {
   Carve c{static_cast<char*>(ws)};
   BwdWork w;
-  w.norms = c.take<uint32_t>(2);
+  w.norms = c.take<float>(2 * kNormBlocks);
   w.delta = c.take<float>(row_heads(p));
+  w.lse2 = c.take<float>(row_heads(p));
   w.total = c.off;
   return w;
 }
@@ -318,7 +329,7 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
 
   const int DP = padded_width(p->D, p->C);
   a.s = shape_of(*p, q_index, k_index);
-  a.lse = lse;
+  a.lse2 = w.lse2;
   a.delta = w.delta;
   a.st_sb = p->packed ? 0 : p->Hq * p->M;
   a.st_sh = p->M;
@@ -329,25 +340,30 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
   AttnPrepArgs pr{};
   pr.s = a.s;
   pr.out = ao, pr.low = alow, pr.dout = a.dout, pr.v = a.v;
+  pr.lse = lse;
+  pr.lse2 = w.lse2;
   pr.delta = w.delta;
   pr.st_sb = a.st_sb, pr.st_sh = a.st_sh;
   pr.norms = scaling ? w.norms : nullptr;
   pr.q_units = row_heads(*p);
   pr.k_units = scaling ? B * p->N * p->Hkv : 0;
-  const int64_t q_blocks = (pr.q_units + 15) / 16, k_blocks = (pr.k_units + 15) / 16;
-  pr.q_blocks = (int32_t)q_blocks;
+  // enough workgroups to fill the GPU several times; with norms as many as the
+  // passes read maxima of
+  const int64_t most = scaling ? kNormBlocks : 2048;
+  pr.q_blocks = (int32_t)std::min(most, (pr.q_units + 15) / 16);
+  pr.k_blocks = (int32_t)std::min(most, (pr.k_units + 15) / 16);
+  a.q_blocks = pr.q_blocks, a.k_blocks = pr.k_blocks;
 
   const int64_t q_tiles = tiles_of(*p, p->M, attn_bwd_cols(DP, false)), q_heads = p->Hq * B;
   const int64_t k_tiles = tiles_of(*p, p->N, attn_bwd_cols(DP, true)), k_heads = p->Hkv * B;
-  if (q_tiles * q_heads > kMaxGrid || k_tiles * k_heads > kMaxGrid || q_blocks + k_blocks > kMaxGrid)
+  if (q_tiles * q_heads > kMaxGrid || k_tiles * k_heads > kMaxGrid)
     return GS_ERR_BAD_SHAPE;
 
   hipError_t e = hipSuccess;
-  if (scaling) e = launch(&k_attn_clear, 1, 64, w.norms, stream);
-  if (e != hipSuccess) return GS_ERR_HIP;
-  e = q_blocks + k_blocks == 0 ? hipSuccess
-      : p->dtype == GS_F16     ? launch(&k_attn_prep<F16>, q_blocks + k_blocks, 256, pr, stream)
-                               : launch(&k_attn_prep<BF16>, q_blocks + k_blocks, 256, pr, stream);
+  const int blocks = pr.q_blocks + pr.k_blocks;
+  if (blocks > 0)
+    e = p->dtype == GS_F16 ? launch(&k_attn_prep<F16>, blocks, 256, pr, stream)
+                           : launch(&k_attn_prep<BF16>, blocks, 256, pr, stream);
   if (e != hipSuccess) return GS_ERR_HIP;
   for (int kv = 0; kv < 2; ++kv) {
     if (kv ? (!dk && !dv) || p->N == 0 : !dq || p->M == 0) continue;

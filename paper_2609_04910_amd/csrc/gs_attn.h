@@ -29,6 +29,7 @@ constexpr int kNoRow = -1;
 constexpr int kRestOut = 1, kRestLse = 2;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr uint32_t kNanPair = 0x7fff7fffu;  // NaN in fp16 and in bf16
 
 // One array of the caller: element (sequence b, row i, head h, column) at
 // p + b*sb + i*sr + h*sh + 2*column (bytes; 4*column for 32-bit data).
@@ -74,6 +75,8 @@ __device__ __forceinline__ AttnSeq seq_of(const AttnShape& s, int b) {
   AttnSeq r;
   seq_side(s.q_index, s.packed, b, s.M, r.q0, r.qn);
   seq_side(s.k_index, s.packed, b, s.N, r.k0, r.kn);
+  r.q0 = __builtin_amdgcn_readfirstlane(r.q0), r.qn = __builtin_amdgcn_readfirstlane(r.qn);
+  r.k0 = __builtin_amdgcn_readfirstlane(r.k0), r.kn = __builtin_amdgcn_readfirstlane(r.kn);
   return r;
 }
 
@@ -176,14 +179,26 @@ __device__ __forceinline__ bool not_finite(const uint4& a) {
 typedef __attribute__((address_space(3))) char attn_lds;
 __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(const attn_lds*)p; }
 
-// 64 lanes x 16 bytes from per-lane addresses to LDS bytes m0 + 16 * lane.
-// Assembly, so that the compiler neither sees nor waits for the copy: the
-// tile loop waits (copies_done) before the barrier that publishes it.  The
-// s_nop separates the write of m0 from its use.
+// 64 lanes x 16 (4) bytes from base + per-lane offset, or from per-lane
+// addresses, to LDS bytes lds + 16 (4) * lane.  Assembly, so that the compiler
+// neither sees nor waits for the copy: the tile loop waits (tile_barrier) before the
+// barrier that publishes it.  The s_nop separates the write of m0 from its use.
+__device__ __forceinline__ void copy16(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(lds), "v"(off), "s"(base)
+               : "memory", "m0");
+}
 __device__ __forceinline__ void copy16(const char* src, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(lds), "v"(src)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void copy4(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(lds), "v"(off), "s"(base)
                : "memory", "m0");
 }
 
@@ -196,39 +211,64 @@ __device__ __forceinline__ void tile_barrier() {
 
 __host__ __device__ constexpr int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
 
-constexpr uint32_t kNanPair = 0x7fff7fffu;  // NaN in fp16 and in bf16
+// A value that is the same in all lanes, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// ROWS rows of DP elements into LDS by THREADS threads.  row(r) gives the address
-// of tile row r (never past the caller's array), or NULL for a row that is read
-// as NaN.
-template <int DP, int ROWS, int THREADS, typename Row>
-__device__ __forceinline__ void load_tile(char* tile, int width, int vec, Row row) {
-  constexpr int NCH = DP / 8;
-  static_assert(ROWS * NCH % THREADS == 0, "whole waves");
-  const int tid = threadIdx.x;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+// This thread's share of a tile of ROWS rows of DP elements that THREADS threads
+// copy: 16-byte chunk `chunk` of rows row0, row0 + STEP, ...
+template <int DP, int ROWS, int THREADS>
+struct TileCopy {
+  static constexpr int NCH = DP / 8, STEP = THREADS / NCH, N = ROWS / STEP;
+  static_assert(THREADS % NCH == 0 && ROWS % STEP == 0 && STEP % 8 == 0, "rows of one swizzle");
+  int row0, chunk;
+  __device__ __forceinline__ TileCopy() {
+    row0 = threadIdx.x / NCH;
+    chunk = (threadIdx.x % NCH) ^ swz(row0);
+  }
+  // LDS bytes of this wave's share of step i
+  __device__ __forceinline__ uint32_t lds(const char* tile, int i) const {
+    return uniform(lds_offset(tile)) + i * THREADS * 16 + uniform(threadIdx.x >> 6) * 1024;
+  }
+
+  // Rows first .. of an array (row `first` at base), none past row `last` of the
+  // tile (that row is repeated: what is past the end is masked).  Rows 16-byte
+  // aligned, a multiple of 8 wide, ROWS * sr below 2^31.
+  __device__ __forceinline__ void wide(char* tile, const char* base, uint32_t sr, int last, int width) const {
+    if (chunk * 8 >= width) return;
 #pragma unroll
-  for (int it = 0; it < ROWS * NCH / THREADS; ++it) {
-    const int at = it * THREADS + tid;
-    const int r = at / NCH, c = (at % NCH) ^ swz(r);
-    const char* src = row(r);
-    if (vec) {
-      if (c * 8 < width) {
-        if (src)
-          copy16(src + c * 16, __builtin_amdgcn_readfirstlane(lds_offset(tile)) + (it * THREADS + wave * 64) * 16);
-        else
-          *reinterpret_cast<uint4*>(tile + at * 16) = uint4{kNanPair, kNanPair, kNanPair, kNanPair};
-      }
-    } else {
+    for (int i = 0; i < N; ++i)
+      copy16(base, (uint32_t)min(row0 + i * STEP, last) * sr + chunk * 16, lds(tile, i));
+  }
+  // Rows anywhere: row(i) is the address of the thread's i-th row, NULL for a row
+  // that reads as NaN.
+  template <typename Row>
+  __device__ __forceinline__ void wide_rows(char* tile, int width, Row row) const {
+    if (chunk * 8 >= width) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const char* src = row(i);
+      if (src)
+        copy16(src + chunk * 16, lds(tile, i));
+      else
+        *reinterpret_cast<uint4*>(tile + (i * THREADS + threadIdx.x) * 16) =
+            uint4{kNanPair, kNanPair, kNanPair, kNanPair};
+    }
+  }
+  // Element by element (any alignment and width).
+  template <typename Row>
+  __device__ __forceinline__ void narrow_rows(char* tile, int width, Row row) const {
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      const char* src = row(i);
       uint32_t x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        x[e] = c * 8 + e >= width ? 0u : src ? reinterpret_cast<const uint16_t*>(src)[c * 8 + e] : 0x7fffu;
-      *reinterpret_cast<uint4*>(tile + at * 16) =
+        x[e] = chunk * 8 + e >= width ? 0u : src ? reinterpret_cast<const uint16_t*>(src)[chunk * 8 + e] : 0x7fffu;
+      *reinterpret_cast<uint4*>(tile + (i * THREADS + threadIdx.x) * 16) =
           uint4{x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
     }
   }
-}
+};
 
 // Zeros over all of a workgroup's tiles: the columns past the caller's width are
 // not written by the copies.
@@ -272,58 +312,74 @@ __device__ __forceinline__ uint4 tr_operand(const char* tile, const TileLane<DP>
   return uint4{a.x, a.y, b.x, b.y};
 }
 
-// f applied to the eight 16-bit elements.
-template <typename F>
-__device__ __forceinline__ uint4 each16(const uint4& a, F f) {
-  auto two = [&](uint32_t x) { return f(x & 0xffffu) | f(x >> 16) << 16; };
-  return uint4{two(a.x), two(a.y), two(a.z), two(a.w)};
+// Nothing moves across: keeps a stage's LDS reads one stage ahead of the
+// matrix instructions that use them.  Left to itself the compiler issues a whole
+// phase's reads at once, and holds them in registers that the sums need (the
+// D = 128 kernels then spilled 50 to 450 values inside the tile loop).
+__device__ __forceinline__ void stage_fence() { __builtin_amdgcn_sched_barrier(0); }
+
+// s[n] += X U[n] over NC chunks of 32 columns: rows 16 t .. of a tile.
+template <typename T, int DP, int NT>
+__device__ __forceinline__ void scores(const char* tile, const TileLane<DP>& ln, int t, const uint4 (&u)[NT][DP / 32],
+                                       floatx4 (&s)[NT]) {
+  constexpr int NC = DP / 32;
+  uint4 x[2];
+  x[0] = row_operand<DP>(tile, ln, t, 0);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    if (c + 1 < NC) x[(c + 1) & 1] = row_operand<DP>(tile, ln, t, c + 1);
+    stage_fence();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n] = mfma_qk<T>(x[c & 1], u[n][c], s[n]);
+    stage_fence();
+  }
 }
 
 // acc[ct][n] += X^T B[n] over the 32 rows of step s of a tile: NC transposed
-// operands, NT column tiles.  Where some columns do not see some rows (masked)
-// B is zero there, but a row with an infinity or NaN may reach only the columns
-// that see it, and 0 * NaN is NaN.  Such elements are then contracted apart:
-// the rest of the operand as it is, and the products' infinities by their signs, as
-// counts of +inf and -inf (an element that is NaN counts as both, and
-// inf - inf is NaN again).
-template <typename T, int DP, bool SIGNED, int NC, int NT>
+// operands, NT column tiles.
+template <typename T, int DP, int NC, int NT>
 __device__ __forceinline__ void contract(const char* tile, const TileLane<DP>& ln, int s, const uint4 (&b)[NT],
-                                         floatx4 (&acc)[NC][NT], bool masked) {
-  constexpr uint32_t e = exponent_bits<T>(), one = __is_same(T, F16) ? 0x3c00u : 0x3f80u;
-  bool apart = false;
-  if (masked) {
-    bool bad = false;
-#pragma unroll
-    for (int ct = 0; ct < NC; ++ct) bad |= not_finite<T>(tr_operand<DP>(tile, ln, s, ct));
-    apart = __any(bad);
-  }
+                                         floatx4 (&acc)[NC][NT]) {
+  uint4 a[2];
+  a[0] = tr_operand<DP>(tile, ln, s, 0);
 #pragma unroll
   for (int ct = 0; ct < NC; ++ct) {
-    uint4 a = tr_operand<DP>(tile, ln, s, ct);
-    if (apart) {
-      const uint4 up = each16(a, [=](uint32_t x) { return (x & e) == e && (x != (e | 0x8000u)) ? one : 0u; });
-      const uint4 down = each16(a, [=](uint32_t x) { return (x & e) == e && x != e ? one : 0u; });
+    if (ct + 1 < NC) a[(ct + 1) & 1] = tr_operand<DP>(tile, ln, s, ct + 1);
+    stage_fence();
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint4 bp = each16(b[n], [=](uint32_t x) { return x != 0 && x < 0x8000u ? one : 0u; });
-        floatx4 inf = mfma_qk<T>(up, bp, floatx4{0, 0, 0, 0}), ninf = mfma_qk<T>(down, bp, floatx4{0, 0, 0, 0});
-        if (SIGNED) {
-          const uint4 bn = each16(b[n], [=](uint32_t x) { return x > 0x8000u ? one : 0u; });
-          inf = mfma_qk<T>(down, bn, inf);
-          ninf = mfma_qk<T>(up, bn, ninf);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          acc[ct][n][r] += inf[r] > 0.0f ? __builtin_inff() : 0.0f;
-          acc[ct][n][r] -= ninf[r] > 0.0f ? __builtin_inff() : 0.0f;
-        }
-      }
-      a = each16(a, [=](uint32_t x) { return (x & e) == e ? 0u : x; });
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[ct][n] = mfma_qk<T>(a, b[n], acc[ct][n]);
+    for (int n = 0; n < NT; ++n) acc[ct][n] = mfma_qk<T>(a[ct & 1], b[n], acc[ct][n]);
+    stage_fence();
   }
 }
+
+// Tiles some of whose rows some columns do not see.  Their weights are zero
+// there, but 0 * NaN is NaN: an infinity or NaN may reach only the columns that
+// see its row.  So each thread zeroes such elements in the chunks of the tile that
+// it copied itself, before the barrier that publishes the tile, and leaves the
+// tile's number in `mark` where there were any; the columns that see those rows
+// are then found apart (a rare path that keeps to a few registers).  Returns
+// whether the thread found any.
+template <typename T, int DP, int ROWS, int THREADS>
+__device__ __forceinline__ bool clean_tile(char* tile) {
+  constexpr uint32_t e = exponent_bits<T>();
+  bool any = false;
+#pragma unroll
+  for (int it = 0; it < ROWS * DP / 8 / THREADS; ++it) {
+    uint4* p = reinterpret_cast<uint4*>(tile + (it * THREADS + threadIdx.x) * 16);
+    const uint4 x = *p;
+    if (not_finite<T>(x)) {
+      auto fix = [](uint32_t y) {
+        return ((y & e) == e ? 0u : y & 0xffffu) | (((y >> 16) & e) == e ? 0u : y & 0xffff0000u);
+      };
+      *p = uint4{fix(x.x), fix(x.y), fix(x.z), fix(x.w)};
+      any = true;
+    }
+  }
+  return any;
+}
+
+// Every copy of this wave's threads has landed (not yet those of other waves).
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // ------------------------------------------------------------- 16-bit output
 

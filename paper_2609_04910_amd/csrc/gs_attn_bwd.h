@@ -15,13 +15,18 @@
 
 namespace gs {
 
+// At most this many workgroups of the preparation look at norms; each writes its
+// own maximum, and the passes take the largest (no atomics, nothing to clear).
+constexpr int kNormBlocks = 256;
+
 struct AttnBwdArgs {
   AttnShape s;
   AttnArray q, k, v, dout, dq, dk, dv;
-  const float* lse;
+  const float* lse2;       // lse log2 e
   const float* delta;
-  int64_t st_sb, st_sh;    // elements: lse and delta of (sequence, head)
-  const uint32_t* norms;   // fp16: bits of the largest row norms of dout and v
+  int64_t st_sb, st_sh;    // elements: lse2 and delta of (sequence, head)
+  const float* norms;      // fp16: largest row norms of dout and (from kNormBlocks on) v
+  int32_t q_blocks, k_blocks;  // and how many there are
   int32_t tiles, heads;    // as in AttnFwdArgs
   float c;                 // scale log2 e
 };
@@ -34,32 +39,41 @@ constexpr int kWeightShift = 15;
 template <typename T>
 constexpr bool scaled() { return __is_same(T, F16); }
 
-__device__ __forceinline__ int ds_exponent(const uint32_t* norms) {
-  const float x = __builtin_bit_cast(float, norms[0]), y = __builtin_bit_cast(float, norms[1]);
-  const float z = x * y;
+__device__ __forceinline__ int ds_exponent(const float* norms, int q_blocks, int k_blocks) {
+  float z = 1.0f;
+  for (int side = 0; side < 2; ++side) {
+    float m = 0.0f;
+    const int n = side ? k_blocks : q_blocks;
+    for (int i = threadIdx.x & 63; i < n; i += 64) {
+      const float x = norms[side * kNormBlocks + i];
+      m = x <= m ? m : x;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const float x = __shfl_xor(m, d);
+      m = x <= m ? m : x;
+    }
+    z *= m;
+  }
   if (!(z > 0.0f) || !(z < __builtin_inff())) return 0;
   int e;
   (void)frexpf(z, &e);  // z < 2^e
-  return clampi(14 - e, -100, 100);
+  return uniform(clampi(14 - e, -100, 100));
 }
 
-// delta, and for fp16 the largest row norms of dout (norms[0]) and v (norms[1])
-// over the rows in use.  16 lanes a row and head; a maximum of non-negative
-// numbers by their bits does not depend on its order.
-template <typename T>
-__device__ __forceinline__ float elem(const char* row, int c) {
-  return T::to_float(reinterpret_cast<const uint16_t*>(row)[c]);
-}
-
+// lse in log2 units, delta, and for fp16 the largest row norms of dout and v over
+// the rows in use.  16 lanes a row and head; bound by reading dout and out.
 struct AttnPrepArgs {
   AttnShape s;
   AttnArray out, low, dout, v;  // low.p may be NULL
+  const float* lse;
+  float* lse2;
   float* delta;
   int64_t st_sb, st_sh;
-  uint32_t* norms;      // NULL: not wanted
-  int64_t q_units;      // rows x query heads, all sequences (padded to whole workgroups by the grid)
+  float* norms;         // NULL: not wanted
+  int64_t q_units;      // rows x query heads, all sequences
   int64_t k_units;      // rows x key heads (0: no norms)
-  int32_t q_blocks;
+  int32_t q_blocks, k_blocks;
 };
 
 __device__ __forceinline__ bool row_used(const int32_t* index, int packed, int b, int i, int rows, int B) {
@@ -68,56 +82,103 @@ __device__ __forceinline__ bool row_used(const int32_t* index, int packed, int b
   return B > 0 && i >= index[0] && i < index[B];
 }
 
+// Columns 8 lane .. of a row (16 lanes a row) as fp32, zero past the width.
+template <typename T>
+__device__ __forceinline__ void row8(const char* row, int vec, int width, int c, float (&x)[8]) {
+  uint32_t y[8];
+  if (vec) {
+    uint4 z{0, 0, 0, 0};
+    if (c < width) z = *reinterpret_cast<const uint4*>(row + 2 * c);
+    const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = c + e < width ? reinterpret_cast<const uint16_t*>(row)[c + e] : 0u;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = T::to_float((uint16_t)y[e]);
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_prep(const AttnPrepArgs a) {
+  __shared__ float wave_max[4];
   const AttnShape& s = a.s;
   const int lane = threadIdx.x & 15;
   const bool keys = (int)blockIdx.x >= a.q_blocks;
-  const int64_t unit = (int64_t)(blockIdx.x - (keys ? a.q_blocks : 0)) * 16 + (threadIdx.x >> 4);
+  const int block = keys ? (int)blockIdx.x - a.q_blocks : (int)blockIdx.x;
+  const int64_t units = keys ? a.k_units : a.q_units, stride = (int64_t)(keys ? a.k_blocks : a.q_blocks) * 16;
+  const int H = keys ? s.Hkv : s.Hq, R = keys ? s.N : s.M;
   float norm = 0.0f;
-  if (unit < (keys ? a.k_units : a.q_units)) {
-    const int H = keys ? s.Hkv : s.Hq, R = keys ? s.N : s.M;
+  for (int64_t unit = (int64_t)block * 16 + (threadIdx.x >> 4); unit < units; unit += stride) {
     const int h = (int)(unit % H);
     const int64_t row = unit / H;
     const int b = s.packed ? 0 : (int)(row / R), i = s.packed ? (int)row : (int)(row % R);
-    const bool used = row_used(keys ? s.k_index : s.q_index, s.packed, b, i, R, s.B);
     float dot = 0.0f, sq = 0.0f;
-    if (keys) {
-      const char* p = a.v.p + b * a.v.sb + i * a.v.sr + h * a.v.sh;
-      for (int c = lane; c < s.C; c += 16) {
-        const float x = elem<T>(p, c);
-        sq = __builtin_fmaf(x, x, sq);
+    for (int c = 8 * lane; c < s.C; c += 128) {
+      float x[8];
+      if (keys) {
+        row8<T>(a.v.p + b * a.v.sb + i * a.v.sr + h * a.v.sh, a.v.vec, s.C, c, x);
+      } else {
+        float o[8];
+        row8<T>(a.dout.p + b * a.dout.sb + i * a.dout.sr + h * a.dout.sh, a.dout.vec, s.C, c, x);
+        row8<T>(a.out.p + b * a.out.sb + i * a.out.sr + h * a.out.sh, a.out.vec, s.C, c, o);
+        if (a.low.p) {
+          float l[8];
+          row8<T>(a.low.p + b * a.low.sb + i * a.low.sr + h * a.low.sh, a.low.vec, s.C, c, l);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] += l[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(x[e], o[e], dot);
       }
-    } else {
-      const char* p = a.dout.p + b * a.dout.sb + i * a.dout.sr + h * a.dout.sh;
-      const char* o = a.out.p + b * a.out.sb + i * a.out.sr + h * a.out.sh;
-      const char* ol = a.low.p ? a.low.p + b * a.low.sb + i * a.low.sr + h * a.low.sh : nullptr;
-      for (int c = lane; c < s.C; c += 16) {
-        const float x = elem<T>(p, c);
-        sq = __builtin_fmaf(x, x, sq);
-        dot = __builtin_fmaf(x, elem<T>(o, c) + (ol ? elem<T>(ol, c) : 0.0f), dot);
-      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(x[e], x[e], sq);
     }
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) {
       sq += __shfl_xor(sq, d);
       dot += __shfl_xor(dot, d);
     }
-    if (!keys && lane == 0) a.delta[b * a.st_sb + h * a.st_sh + i] = dot;
-    norm = used ? __builtin_sqrtf(sq) : 0.0f;
+    if (!keys && lane == 0) {
+      const int64_t at = b * a.st_sb + h * a.st_sh + i;
+      a.delta[at] = dot;
+      a.lse2[at] = a.lse[at] * kLog2e;
+    }
+    if (a.norms && row_used(keys ? s.k_index : s.q_index, s.packed, b, i, R, s.B)) {
+      const float z = __builtin_sqrtf(sq);
+      norm = z <= norm ? norm : z;  // a NaN stays
+    }
   }
   if (a.norms) {
 #pragma unroll
-    for (int d = 16; d < 64; d <<= 1) norm = fmaxf(norm, __shfl_xor(norm, d));
-    if ((threadIdx.x & 63) == 0 && norm > 0.0f) atomicMax(a.norms + keys, __builtin_bit_cast(uint32_t, norm));
+    for (int d = 16; d < 64; d <<= 1) {
+      const float z = __shfl_xor(norm, d);
+      norm = z <= norm ? norm : z;
+    }
+    if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = norm;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < 4; ++w) norm = wave_max[w] <= norm ? norm : wave_max[w];
+      a.norms[(keys ? kNormBlocks : 0) + block] = norm;
+    }
   }
 }
 
-template <typename T, int DP, int NT, int NW, bool KV>
+template <typename T>
+__device__ __forceinline__ bool row_not_finite(const char* row, int width) {
+  constexpr uint32_t e = exponent_bits<T>();
+  bool bad = false;
+  for (int c = 0; c < width; ++c) bad |= (reinterpret_cast<const uint16_t*>(row)[c] & e) == e;
+  return bad;
+}
+
+template <typename T, int DP, int NT, int NW, bool KV, bool WIDE>
 __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
   constexpr int BR = attn_keys<DP>(), NC = DP / 32, NO = DP / 16, TILE = BR * DP * 2, COLS = 16 * NT * NW;
   __shared__ __align__(1024) char smem[4 * TILE];
   __shared__ __align__(16) float stat[2][2][BR];  // [stage][lse, delta][row]
+  __shared__ int mark[4];
   const AttnShape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
@@ -184,16 +245,16 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       }
       if (!KV) {
         const int64_t i = b * a.st_sb + head * a.st_sh + c0 + at;
-        clse[n] = a.lse[i] * kLog2e;
+        clse[n] = a.lse2[i];
         cdelta[n] = a.delta[i];
       }
     }
   }
   int r_lo = 0, r_hi = 0, w_lo = 0, w_hi = 0, in_lo = 0, in_hi = 0;
+  int all_lo = 0, all_hi = 0;  // rows that every column of the workgroup sees
   if (cn > 0 && t0 < cn) {
-    int x;
-    range(t0, r_lo, x);
-    range(min(t0 + COLS, cn) - 1, x, r_hi);
+    range(t0, r_lo, all_hi);
+    range(min(t0 + COLS, cn) - 1, all_lo, r_hi);
     range(min(wc0, cn - 1), w_lo, in_hi);
     range(min(wc0 + 16 * NT, cn) - 1, in_lo, w_hi);
     if (wc0 >= cn) w_hi = w_lo = 0;
@@ -208,76 +269,94 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       du[ct][n] = floatx4{0, 0, 0, 0};
       if (KV) dw[ct][n] = floatx4{0, 0, 0, 0};
     }
-  const int ds_e = scaled<T>() ? ds_exponent(a.norms) : 0;
+  const int ds_e = scaled<T>() ? ds_exponent(a.norms, a.q_blocks, a.k_blocks) : 0;
   const float ds_up = __builtin_ldexpf(1.0f, ds_e);
 
   const TileLane<DP> ln;
   // the stream: tiles of rows [r_lo, r_hi), once for every query head (KV)
   const int heads = KV ? s.G : 1, h0 = KV ? head * s.G : head / s.G;
   const int steps = r_hi > r_lo ? (r_hi - r_lo + BR - 1) / BR : 0;
+  const TileCopy<DP, BR, 64 * NW> tc;
   auto issue = [&](int h, int row0, int stage) {
     char* t = smem + stage * 2 * TILE;
     const char* xb = X.p + b * X.sb + (int64_t)x0 * X.sr + (h0 + h) * X.sh;
     const char* yb = Y.p + b * Y.sb + (int64_t)x0 * Y.sr + (h0 + h) * Y.sh;
-    load_tile<DP, BR, 64 * NW>(t, s.D, X.vec, [&](int r) { return xb + (int64_t)min(row0 + r, rn - 1) * X.sr; });
-    load_tile<DP, BR, 64 * NW>(t + TILE, s.C, Y.vec,
-                               [&](int r) { return yb + (int64_t)min(row0 + r, rn - 1) * Y.sr; });
-    if (KV && tid < BR) {
-      const int64_t i = b * a.st_sb + (h0 + h) * a.st_sh + x0 + min(row0 + tid, rn - 1);
-      stat[stage][0][tid] = a.lse[i] * kLog2e;
-      stat[stage][1][tid] = a.delta[i];
+    if constexpr (WIDE) {
+      tc.wide(t, xb + (int64_t)row0 * X.sr, (uint32_t)X.sr, rn - 1 - row0, s.D);
+      tc.wide(t + TILE, yb + (int64_t)row0 * Y.sr, (uint32_t)Y.sr, rn - 1 - row0, s.C);
+    } else {
+      auto row_of = [&](int i) { return min(row0 + tc.row0 + i * tc.STEP, rn - 1); };
+      tc.narrow_rows(t, s.D, [&](int i) { return xb + (int64_t)row_of(i) * X.sr; });
+      tc.narrow_rows(t + TILE, s.C, [&](int i) { return yb + (int64_t)row_of(i) * Y.sr; });
+    }
+    if (KV && wave < 2 && lane < BR) {  // the first wave copies lse, the second delta
+      const float* p = (wave ? a.delta : a.lse2) + b * a.st_sb + (h0 + h) * a.st_sh + x0 + row0;
+      copy4(p, min(lane, rn - 1 - row0) * 4, uniform(lds_offset(stat[stage][wave])));
     }
   };
   if (s.D < DP || s.C < DP) {
     clear_tiles<64 * NW>(smem, 4 * TILE);
     __syncthreads();
   }
+  // columns that see a row with an infinity or NaN: their gradients are NaN
+  bool spoilt[NT] = {};
   if (steps > 0) issue(0, r_lo, 0);
-  int stage = 0;
+  int stage = 0, it = 0;
   for (int h = 0; h < heads; ++h)
     for (int st = 0; st < steps; ++st, stage ^= 1) {
+      ++it;
+      const int row0 = r_lo + st * BR;
+      const bool bordered = row0 + BR > all_hi || row0 < all_lo;
+      if (bordered) {
+        copies_done();
+        char* t = smem + stage * 2 * TILE;
+        if (clean_tile<T, DP, BR, 64 * NW>(t) | clean_tile<T, DP, BR, 64 * NW>(t + TILE)) mark[it & 3] = it;
+      }
       tile_barrier();
       if (st + 1 < steps)
         issue(h, r_lo + (st + 1) * BR, stage ^ 1);
       else if (h + 1 < heads)
         issue(h + 1, r_lo, stage ^ 1);
-      const int row0 = r_lo + st * BR;
+      if (bordered && uniform(mark[it & 3]) == it) {
+        const int at = min(row0 + lane, rn - 1);
+        const char* xr = X.p + b * X.sb + (int64_t)(x0 + at) * X.sr + (h0 + h) * X.sh;
+        const char* yr = Y.p + b * Y.sb + (int64_t)(x0 + at) * Y.sr + (h0 + h) * Y.sh;
+        const bool own = lane < BR && row0 + lane < rn;
+        const uint64_t bad = __ballot(own && (row_not_finite<T>(xr, s.D) || row_not_finite<T>(yr, s.C)));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int f = clampi(lo[n] - row0, 0, BR), l = clampi(hi[n] - row0, f, BR);
+          const uint64_t seen = (l == 64 ? ~0ull : (1ull << l) - 1) & ~(f == 64 ? ~0ull : (1ull << f) - 1);
+          spoilt[n] |= (bad & seen) != 0;
+        }
+      }
       if (row0 >= w_hi || row0 + BR <= w_lo) continue;
       const char* xt = smem + stage * 2 * TILE;
       const char* yt = xt + TILE;
       const bool masked = row0 + BR > in_hi || row0 < in_lo;
 #pragma unroll
       for (int hf = 0; hf < BR / 32; ++hf) {
-        uint4 pw[NT], dsw[NT];
-        floatx4 sc[2][NT], dp[2][NT];
+        uint32_t pw[NT][4], dsw[NT][4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+          floatx4 sc[NT], dp[NT];
+          floatx4 rl{0, 0, 0, 0};
+          // dP - delta: the sums start at -delta
 #pragma unroll
-          for (int n = 0; n < NT; ++n) sc[t][n] = dp[t][n] = floatx4{0, 0, 0, 0};
-#pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            const uint4 xo = row_operand<DP>(xt, ln, 2 * hf + t, c);
-            const uint4 yo = row_operand<DP>(yt, ln, 2 * hf + t, c);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              sc[t][n] = mfma_qk<T>(xo, uo[n][c], sc[t][n]);
-              dp[t][n] = mfma_qk<T>(yo, wo[n][c], dp[t][n]);
-            }
+          for (int n = 0; n < NT; ++n) {
+            sc[n] = floatx4{0, 0, 0, 0};
+            dp[n] = KV ? -*reinterpret_cast<const floatx4*>(&stat[stage][1][32 * hf + 16 * t + 4 * g])
+                       : floatx4{-cdelta[n], -cdelta[n], -cdelta[n], -cdelta[n]};
           }
-        }
+          if (KV) rl = *reinterpret_cast<const floatx4*>(&stat[stage][0][32 * hf + 16 * t + 4 * g]);
+          scores<T, DP, NT>(xt, ln, 2 * hf + t, uo, sc);
+          scores<T, DP, NT>(yt, ln, 2 * hf + t, wo, dp);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          floatx4 rl{0, 0, 0, 0}, rd{0, 0, 0, 0};
-          if (KV) {
-            rl = *reinterpret_cast<const floatx4*>(&stat[stage][0][32 * hf + 16 * t + 4 * g]);
-            rd = *reinterpret_cast<const floatx4*>(&stat[stage][1][32 * hf + 16 * t + 4 * g]);
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][n][r], a.c, -(KV ? rl[r] : clse[n])));
-              float d = p * (dp[t][n][r] - (KV ? rd[r] : cdelta[n]));
+              float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r], a.c, -(KV ? rl[r] : clse[n])));
+              float d = p * dp[n][r];
               if (masked) {
                 const int j = row0 + 32 * hf + 16 * t + 4 * g + r;
                 const bool in = j >= lo[n] && j < hi[n];
@@ -285,19 +364,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
                 d = in ? d : 0.0f;
               }
               // the weights and dS are rounded to the inputs' type for the matrix cores
-              sc[t][n][r] = scaled<T>() ? p * (float)(1 << kWeightShift) : p;
-              dp[t][n][r] = scaled<T>() ? d * ds_up : d;
+              sc[n][r] = scaled<T>() ? p * (float)(1 << kWeightShift) : p;
+              dp[n][r] = scaled<T>() ? d * ds_up : d;
             }
+            pw[n][2 * t] = pack2<T>(sc[n][0], sc[n][1]);
+            pw[n][2 * t + 1] = pack2<T>(sc[n][2], sc[n][3]);
+            dsw[n][2 * t] = pack2<T>(dp[n][0], dp[n][1]);
+            dsw[n][2 * t + 1] = pack2<T>(dp[n][2], dp[n][3]);
+          }
         }
+        uint4 pb[NT], db[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          pw[n] = uint4{pack2<T>(sc[0][n][0], sc[0][n][1]), pack2<T>(sc[0][n][2], sc[0][n][3]),
-                        pack2<T>(sc[1][n][0], sc[1][n][1]), pack2<T>(sc[1][n][2], sc[1][n][3])};
-          dsw[n] = uint4{pack2<T>(dp[0][n][0], dp[0][n][1]), pack2<T>(dp[0][n][2], dp[0][n][3]),
-                         pack2<T>(dp[1][n][0], dp[1][n][1]), pack2<T>(dp[1][n][2], dp[1][n][3])};
+          pb[n] = uint4{pw[n][0], pw[n][1], pw[n][2], pw[n][3]};
+          db[n] = uint4{dsw[n][0], dsw[n][1], dsw[n][2], dsw[n][3]};
         }
-        if constexpr (KV) contract<T, DP, false, NO, NT>(yt, ln, hf, pw, dw, masked);
-        contract<T, DP, true, NO, NT>(xt, ln, hf, dsw, du, masked);
+        if constexpr (KV) contract<T, DP>(yt, ln, hf, pb, dw);
+        contract<T, DP>(xt, ln, hf, db, du);
       }
     }
 
@@ -314,6 +397,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
 #pragma unroll
       for (int ct = 0; ct < NO; ++ct) {
         floatx4 y = du[ct][n] * u_scale;
+        if (spoilt[n]) y = floatx4{1, 1, 1, 1} * __builtin_nanf("");
         if (none) y = floatx4{0, 0, 0, 0};
         store4<T>(p, 16 * ct + 4 * g, s.D, DU.vec, y[0], y[1], y[2], y[3]);
       }
@@ -323,6 +407,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
 #pragma unroll
       for (int ct = 0; ct < NO; ++ct) {
         floatx4 y = dw[KV ? ct : 0][n] * w_scale;
+        if (spoilt[n]) y = floatx4{1, 1, 1, 1} * __builtin_nanf("");
         if (none) y = floatx4{0, 0, 0, 0};
         store4<T>(p, 16 * ct + 4 * g, s.C, a.dv.vec, y[0], y[1], y[2], y[3]);
       }
