@@ -10,7 +10,7 @@ Entry points (the C names without their ``gs_`` prefix):
   attention_bwd(q, k, v, out, lse, dout, ...)        -> dq, dk, dv
   attention_append(k, v, k_pages, v_pages, page_table, seq_lens, ...)
   attention_paged(q, k_pages, v_pages, page_table, seq_lens, ...) -> out
-  attention_bwd_workspace_size / attention_paged_workspace_size
+  attention_fwd_workspace_size / attention_bwd_workspace_size / attention_paged_workspace_size
 and ``attention(q, k, v, ...)`` is the forward call under autograd.
 
 Layouts.  Dense: q is B x M x Hq x D, k is B x N x Hkv x D, v is B x N x Hkv x C,
@@ -216,8 +216,10 @@ def _check_like_out(t, name, c, q):
     _check_columns(name, t, len(c.out_shape))
 
 
-def _fwd(c, q, k, v, out, lse, low, stream):
+def _fwd(c, q, k, v, out, lse, low, workspace, stream):
     import torch
+    need = int(load().gs_attention_fwd_workspace_size(_ref(c.problem)))
+    workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
     rest = 0
     if out is None:
         rest = REST_OUT
@@ -232,13 +234,14 @@ def _fwd(c, q, k, v, out, lse, low, stream):
     c.problem.zero_rest = rest
     _launch("gs_attention_fwd", q.device, stream, _ref(c.problem), _ref(_array(q, c.packed)),
             _ref(_array(k, c.packed)), _ref(_array(v, c.packed)), gs._ptr(c.index[0]), gs._ptr(c.index[1]),
-            _ref(_array(out, c.packed)), _ref(_array(low, c.packed)), gs._ptr(lse), None, 0)
-    gs._keep_alive(stream, out, lse)
+            _ref(_array(out, c.packed)), _ref(_array(low, c.packed)), gs._ptr(lse), gs._ptr(workspace),
+            wbytes)
+    gs._keep_alive(stream, out, lse, workspace)
     return out, lse
 
 
 def attention_fwd(q, k, v, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None, q_lens=None,
-                  k_lens=None, out=None, lse=None, low=None, stream=None):
+                  k_lens=None, out=None, lse=None, low=None, workspace=None, stream=None):
     """(out, lse): out_m = sum_n w_mn v_n / sum_n w_mn with w_mn = exp(scale q_m.k_n) over the
     keys that row m sees, lse_m = log sum_n w_mn.
 
@@ -249,7 +252,13 @@ def attention_fwd(q, k, v, scale=None, causal=False, window=0, q_offsets=None, k
     c = _Call(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
     if low is not None:
         _check_like_out(low, "low", c, q)
-    return _fwd(c, q, k, v, out, lse, low, stream)
+    return _fwd(c, q, k, v, out, lse, low, workspace, stream)
+
+
+def attention_fwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed=False):
+    """Workspace bytes of attention_fwd (packed: M and N are the rows of all sequences)."""
+    p = Problem(B, M, N, Hq, Hkv, D, C, 0, dtype, int(packed), 0, 0, 1.0)
+    return int(load().gs_attention_fwd_workspace_size(_ref(p)))
 
 
 def attention_bwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed=False,
@@ -295,7 +304,7 @@ def _make_autograd():
         @staticmethod
         def forward(ctx, q, k, v, call):
             low = torch.empty(call.out_shape, dtype=q.dtype, device=q.device) if any(ctx.needs_input_grad) else None
-            out, lse = _fwd(call, q, k, v, None, None, low, None)
+            out, lse = _fwd(call, q, k, v, None, None, low, None, None)
             ctx.save_for_backward(q, k, v, out, lse, low, *(t for t in call.index if t is not None))
             ctx.call = call
             return out

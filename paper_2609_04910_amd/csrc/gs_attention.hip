@@ -35,6 +35,11 @@ constexpr int kAttnWaves = 4;
 constexpr int attn_nq(int DP) { return DP == 256 ? 1 : DP == 128 ? 3 : 2; }
 constexpr int attn_nt(int DP, bool KV) { return DP == 256 || (KV && DP == 128) ? 1 : 2; }
 
+// Few rows (k_attn_rows): one tile of 16 rows or four (DP = 256: one; four do not
+// fit the registers), and as many waves as their rings fit in LDS.
+constexpr int rows_waves(int DP) { return DP == 256 ? 2 : 4; }
+constexpr int rows_most(int DP) { return DP == 256 ? 16 : 64; }
+
 constexpr int attn_fwd_rows(int DP) { return 16 * kAttnWaves * attn_nq(DP); }
 constexpr int attn_bwd_cols(int DP, bool KV) { return 16 * kAttnWaves * attn_nt(DP, KV); }
 
@@ -44,20 +49,38 @@ hipError_t launch(K kernel, int64_t grid, int threads, const A& args, hipStream_
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(threads), p, 0, st);
 }
 
+// rows: rows of a tile; at most rows_most(DP): k_attn_rows
 template <typename T, int DP>
-hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int64_t grid, hipStream_t st);
+hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int rows, int64_t grid, hipStream_t st);
 template <typename T, int DP>
 hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st);
 
 #if GS_PART != 0
-template <typename T, int DP>
-hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int64_t grid, hipStream_t st) {
-  constexpr int NQ = attn_nq(DP), NW = kAttnWaves;
-  const bool wide = a.k.vec && a.v.vec;
-  return launch(paged ? wide ? &k_attn_fwd<T, DP, NQ, NW, true, true> : &k_attn_fwd<T, DP, NQ, NW, true, false>
-                : wide ? &k_attn_fwd<T, DP, NQ, NW, false, true>
-                       : &k_attn_fwd<T, DP, NQ, NW, false, false>,
+template <typename T, int DP, int NQ, bool PAGED>
+hipError_t attn_rows(const AttnFwdArgs& a, int64_t grid, hipStream_t st) {
+  constexpr int NW = rows_waves(DP);
+  return launch(a.k.vec && a.v.vec ? &k_attn_rows<T, DP, NQ, NW, PAGED, true> : &k_attn_rows<T, DP, NQ, NW, PAGED, false>,
                 grid, 64 * NW, a, st);
+}
+template <typename T, int DP>
+hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int rows, int64_t grid, hipStream_t st) {
+  constexpr int NQ = attn_nq(DP), NW = kAttnWaves;
+  hipError_t e;
+  if (rows <= rows_most(DP)) {
+    constexpr int MOST = rows_most(DP) / 16;
+    e = rows == 16 ? paged ? attn_rows<T, DP, 1, true>(a, grid, st) : attn_rows<T, DP, 1, false>(a, grid, st)
+        : paged    ? attn_rows<T, DP, MOST, true>(a, grid, st)
+                   : attn_rows<T, DP, MOST, false>(a, grid, st);
+  } else {
+    const bool wide = a.k.vec && a.v.vec;
+    e = launch(paged ? wide ? &k_attn_fwd<T, DP, NQ, NW, true, true> : &k_attn_fwd<T, DP, NQ, NW, true, false>
+               : wide ? &k_attn_fwd<T, DP, NQ, NW, false, true>
+                      : &k_attn_fwd<T, DP, NQ, NW, false, false>,
+               grid, 64 * NW, a, st);
+  }
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t units = (int64_t)(a.s.packed ? 1 : a.s.B) * a.s.M * a.s.Hq;
+  return launch(&k_attn_join<T>, (units + 3) / 4, 256, a, st);
 }
 template <typename T, int DP>
 hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st) {
@@ -69,7 +92,7 @@ hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st)
                 grid, 64 * NW, a, st);
 }
 #define GS_ATTN_INSTANCE(T, DP)                                                               \
-  template hipError_t attn_fwd<T, DP>(const AttnFwdArgs&, bool, int64_t, hipStream_t);        \
+  template hipError_t attn_fwd<T, DP>(const AttnFwdArgs&, bool, int, int64_t, hipStream_t);   \
   template hipError_t attn_bwd<T, DP>(const AttnBwdArgs&, bool, int64_t, hipStream_t);
 #if GS_PART == 1 || GS_PART == -1
 GS_ATTN_INSTANCE(F16, 64)
@@ -200,12 +223,59 @@ struct Carve {
   }
 };
 
-struct BwdWork {
-  float *norms, *delta, *lse2;
+// How a forward call is laid out: rows of a tile, query heads packed into the rows
+// of a token, tiles and heads of the grid, parts of a row's keys, workspace.
+struct FwdPlan {
+  int rows;
+  int64_t per, tiles, heads, splits, grid;
+  float *part_o, *part_z;
   size_t total;
 };
 
 int64_t row_heads(const gs_attention_problem& p) { return (p.packed ? 1 : p.B) * p.M * p.Hq; }
+
+// keys: of a sequence, at most (pages) or on average (packed).
+FwdPlan fwd_plan(const gs_attention_problem& p, bool paged, int64_t keys, void* ws) {
+  FwdPlan f{};
+  const int DP = padded_width(p.D, p.C);
+  const int64_t G = p.Hq / p.Hkv, B = p.packed ? 1 : p.B;
+  // rows that share a key head: with the query heads of a token packed, keys and
+  // values are read once for all of them
+  const int64_t shared = (p.packed && p.B > 0 ? (p.M + p.B - 1) / p.B : p.M) * G;
+  const bool few = shared <= rows_most(DP);
+  f.per = paged || few ? G : 1;
+  f.rows = !few ? attn_fwd_rows(DP) : shared <= 16 ? 16 : rows_most(DP);
+  f.tiles = tiles_of(p, p.M * f.per, f.rows);
+  f.heads = (f.per > 1 || G == 1 ? p.Hkv : p.Hq) * B;
+  // With few workgroups a row's keys are cut into parts, none shorter than 256:
+  // k_attn_rows up to 1024 workgroups, four a CU, so that sequences of unequal
+  // length even out; k_attn_fwd to 512, two a CU
+  const int64_t wgs = f.tiles * f.heads, want = few ? 1024 : 512;
+  f.splits = wgs > 0 ? std::max<int64_t>(1, std::min({want / wgs, keys / 256, (int64_t)64})) : 1;
+  f.grid = wgs * f.splits;
+  if (f.splits > 1) {
+    Carve c{static_cast<char*>(ws)};
+    f.part_o = c.take<float>(f.splits * row_heads(p) * p.C);
+    f.part_z = c.take<float>(f.splits * row_heads(p) * 2);
+    f.total = c.off;
+  }
+  return f;
+}
+
+int64_t dense_keys(const gs_attention_problem& p) { return p.packed && p.B > 0 ? p.N / p.B : p.N; }
+int64_t cache_keys(const gs_attention_cache& c) { return std::min(c.table_width * c.page_size, kMaxRows); }
+
+void plan_args(const FwdPlan& f, const gs_attention_problem& p, AttnFwdArgs& a) {
+  a.per = (int32_t)f.per, a.tiles = (int32_t)f.tiles, a.heads = (int32_t)f.heads;
+  a.splits = (int32_t)f.splits, a.part_o = f.part_o, a.part_z = f.part_z;
+  a.neg = p.scale < 0;
+  a.c = forward_factor(p.scale);
+}
+
+struct BwdWork {
+  float *norms, *delta, *lse2;
+  size_t total;
+};
 
 BwdWork bwd_work(const gs_attention_problem& p, void* ws) {
   Carve c{static_cast<char*>(ws)};
@@ -258,16 +328,19 @@ gs_status index_args(const gs_attention_problem& p, const int32_t* q_index, cons
 
 gs_status run_fwd(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_array* k,
                   const gs_attention_array* v, const int32_t* q_index, const int32_t* k_index,
-                  const gs_attention_array* out, const gs_attention_array* low, float* lse, hipStream_t stream) {
+                  const gs_attention_array* out, const gs_attention_array* low, float* lse, void* ws, size_t ws_bytes,
+                  hipStream_t stream) {
   gs_status st = check(p);
   if (st != GS_SUCCESS) return st;
   if (p->B == 0 || p->M == 0) return GS_SUCCESS;
   if ((st = index_args(*p, q_index, k_index)) != GS_SUCCESS) return st;
   const int64_t B = p->packed ? 1 : p->B;
-  const int64_t tiles = tiles_of(*p, p->M, attn_fwd_rows(padded_width(p->D, p->C))), heads = p->Hq * B;
-  if (tiles * heads > kMaxGrid) return GS_ERR_BAD_SHAPE;
+  const FwdPlan f = fwd_plan(*p, false, dense_keys(*p), ws);
+  if (f.grid > kMaxGrid) return GS_ERR_BAD_SHAPE;
+  if ((st = check_workspace(ws, ws_bytes, f.total)) != GS_SUCCESS) return st;
   AttnFwdArgs a{};
-  Span in[5], o[3];
+  Span in[5], o[4];
+  o[3] = span_of(ws, (int64_t)f.total);
   if ((st = array_of(q, B, p->M, p->Hq, p->D, false, a.q, in[0])) != GS_SUCCESS ||
       (low && (st = array_of(low, B, p->M, p->Hq, p->C, true, a.low, o[2])) != GS_SUCCESS) ||
       (st = array_of(k, B, p->N, p->Hkv, p->D, false, a.k, in[1])) != GS_SUCCESS ||
@@ -277,18 +350,15 @@ gs_status run_fwd(const gs_attention_problem* p, const gs_attention_array* q, co
   if (reinterpret_cast<uintptr_t>(lse) & 3) return GS_ERR_MISALIGNED;
   if (lse) o[1] = span_of(lse, 4 * row_heads(*p));
   in[3] = index_span(*p, q_index), in[4] = index_span(*p, k_index);
-  if (overlaps(o, 3, in, 5)) return GS_ERR_ALIAS;
+  if (overlaps(o, 4, in, 5)) return GS_ERR_ALIAS;
 
   a.s = shape_of(*p, q_index, k_index);
   a.lse = lse;
   a.lse_sb = p->packed ? 0 : p->Hq * p->M;
   a.lse_sh = p->M;
-  a.per = 1;
-  a.tiles = (int32_t)tiles, a.heads = (int32_t)heads;
-  a.neg = p->scale < 0;
-  a.c = forward_factor(p->scale);
+  plan_args(f, *p, a);
   const hipError_t e = by_type(*p, [&](auto t, auto dp) {
-    return attn_fwd<decltype(t), decltype(dp)::value>(a, false, tiles * heads, stream);
+    return attn_fwd<decltype(t), decltype(dp)::value>(a, false, f.rows, f.grid, stream);
   });
   return e == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
 }
@@ -408,7 +478,8 @@ gs_status cache_of(const gs_attention_problem& p, const gs_attention_cache* c, b
 }
 
 gs_status run_paged(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_cache* cache,
-                    const int32_t* q_index, const gs_attention_array* out, float* lse, hipStream_t stream) {
+                    const int32_t* q_index, const gs_attention_array* out, float* lse, void* ws, size_t ws_bytes,
+                    hipStream_t stream) {
   gs_status st = check(p);
   if (st != GS_SUCCESS) return st;
   if (!p->causal) return GS_ERR_UNSUPPORTED;
@@ -417,7 +488,7 @@ gs_status run_paged(const gs_attention_problem* p, const gs_attention_array* q, 
   if (reinterpret_cast<uintptr_t>(q_index) & 3) return GS_ERR_MISALIGNED;
   const int64_t B = p->packed ? 1 : p->B, G = p->Hq / p->Hkv;
   AttnFwdArgs a{};
-  Span in[6], o[2];
+  Span in[6], o[3];
   if ((st = array_of(q, B, p->M, p->Hq, p->D, false, a.q, in[0])) != GS_SUCCESS ||
       (st = cache_of(*p, cache, false, a.k, a.v, a.pg, in[1], in[2])) != GS_SUCCESS ||
       (st = array_of(out, B, p->M, p->Hq, p->C, true, a.out, o[0])) != GS_SUCCESS)
@@ -427,22 +498,20 @@ gs_status run_paged(const gs_attention_problem* p, const gs_attention_array* q, 
   in[3] = index_span(*p, q_index);
   in[4] = span_of(cache->lens, 4 * p->B);
   in[5] = span_of(cache->table, 4 * p->B * cache->table_width);
-  if (overlaps(o, 2, in, 6)) return GS_ERR_ALIAS;
   if (p->M * G > kMaxRows) return GS_ERR_BAD_SHAPE;
+  const FwdPlan f = fwd_plan(*p, true, cache_keys(*cache), ws);
+  if (f.grid > kMaxGrid) return GS_ERR_BAD_SHAPE;
+  if ((st = check_workspace(ws, ws_bytes, f.total)) != GS_SUCCESS) return st;
+  o[2] = span_of(ws, (int64_t)f.total);
+  if (overlaps(o, 3, in, 6)) return GS_ERR_ALIAS;
 
   a.s = shape_of(*p, q_index, nullptr);
   a.lse = lse;
   a.lse_sb = p->packed ? 0 : p->M;
   a.lse_sh = p->M * B;
-  a.per = (int32_t)G;
-  const int rows = attn_fwd_rows(padded_width(p->D, p->C));
-  const int64_t tiles = tiles_of(*p, p->M * G, rows), heads = p->Hkv * B;
-  if (tiles * heads > kMaxGrid) return GS_ERR_BAD_SHAPE;
-  a.tiles = (int32_t)tiles, a.heads = (int32_t)heads;
-  a.neg = p->scale < 0;
-  a.c = forward_factor(p->scale);
+  plan_args(f, *p, a);
   const hipError_t e = by_type(*p, [&](auto t, auto dp) {
-    return attn_fwd<decltype(t), decltype(dp)::value>(a, true, tiles * heads, stream);
+    return attn_fwd<decltype(t), decltype(dp)::value>(a, true, f.rows, f.grid, stream);
   });
   return e == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
 }
@@ -482,16 +551,15 @@ gs_status run_append(const gs_attention_problem* p, const gs_attention_array* k,
 extern "C" {
 
 size_t gs_attention_fwd_workspace_size(const gs_attention_problem* p) {
-  (void)p;
-  return 0;
+  if (gs::check(p) != GS_SUCCESS || p->B == 0 || p->M == 0) return 0;
+  return gs::fwd_plan(*p, false, gs::dense_keys(*p), nullptr).total;
 }
 
 gs_status gs_attention_fwd(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_array* k,
                            const gs_attention_array* v, const int32_t* q_index, const int32_t* k_index,
                            const gs_attention_array* out, const gs_attention_array* low, float* lse,
                            void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  (void)workspace, (void)workspace_bytes;
-  return gs::run_fwd(p, q, k, v, q_index, k_index, out, low, lse, stream);
+  return gs::run_fwd(p, q, k, v, q_index, k_index, out, low, lse, workspace, workspace_bytes, stream);
 }
 
 size_t gs_attention_bwd_workspace_size(const gs_attention_problem* p, int want_dq, int want_dk, int want_dv) {
@@ -509,15 +577,16 @@ gs_status gs_attention_bwd(const gs_attention_problem* p, const gs_attention_arr
 }
 
 size_t gs_attention_paged_workspace_size(const gs_attention_problem* p, const gs_attention_cache* cache) {
-  (void)p, (void)cache;
-  return 0;
+  if (gs::check(p) != GS_SUCCESS || !cache || p->B == 0 || p->M == 0 || cache->table_width < 0 ||
+      cache->page_size < 1 || cache->page_size > gs::kMaxRows || cache->table_width > gs::kMaxRows)
+    return 0;
+  return gs::fwd_plan(*p, true, gs::cache_keys(*cache), nullptr).total;
 }
 
 gs_status gs_attention_paged(const gs_attention_problem* p, const gs_attention_array* q,
                              const gs_attention_cache* cache, const int32_t* q_index, const gs_attention_array* out,
                              float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  (void)workspace, (void)workspace_bytes;
-  return gs::run_paged(p, q, cache, q_index, out, lse, stream);
+  return gs::run_paged(p, q, cache, q_index, out, lse, workspace, workspace_bytes, stream);
 }
 
 gs_status gs_attention_append(const gs_attention_problem* p, const gs_attention_array* k,

@@ -29,7 +29,6 @@ constexpr int kNoRow = -1;
 constexpr int kRestOut = 1, kRestLse = 2;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr uint32_t kNanPair = 0x7fff7fffu;  // NaN in fp16 and in bf16
 
 // One array of the caller: element (sequence b, row i, head h, column) at
 // p + b*sb + i*sr + h*sh + 2*column (bytes; 4*column for 32-bit data).
@@ -202,9 +201,17 @@ __device__ __forceinline__ void copy4(const void* base, uint32_t off, uint32_t l
                : "memory", "m0");
 }
 
-// Every copy and LDS access of this wave done, then the workgroup's barrier.
+// At most LEFT copies of this wave still in flight (they complete in order), and
+// no LDS access of it.
+template <int LEFT>
+__device__ __forceinline__ void copies_left() {
+  static_assert(LEFT < 64, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(LEFT) : "memory");
+}
+
+// The workgroup's barrier, with this wave's LDS writes done.
 __device__ __forceinline__ void tile_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -215,43 +222,40 @@ __host__ __device__ constexpr int swz(int row) { return ((row & 3) << 1) | ((row
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // This thread's share of a tile of ROWS rows of DP elements that THREADS threads
-// copy: 16-byte chunk `chunk` of rows row0, row0 + STEP, ...
+// copy: one 16-byte chunk of each of the rows row0 + i * STEP.  (The swizzle only
+// moves bits, and row0 < STEP, so swz(row0 + i * STEP) = swz(row0) ^ swz(i * STEP).)
 template <int DP, int ROWS, int THREADS>
 struct TileCopy {
   static constexpr int NCH = DP / 8, STEP = THREADS / NCH, N = ROWS / STEP;
-  static_assert(THREADS % NCH == 0 && ROWS % STEP == 0 && STEP % 8 == 0, "rows of one swizzle");
-  int row0, chunk;
-  __device__ __forceinline__ TileCopy() {
-    row0 = threadIdx.x / NCH;
-    chunk = (threadIdx.x % NCH) ^ swz(row0);
+  static_assert(THREADS % NCH == 0 && ROWS % STEP == 0 && (STEP & (STEP - 1)) == 0, "whole rows");
+  int tid, row0, chunk0;
+  __device__ __forceinline__ explicit TileCopy(int t) : tid(t) {
+    row0 = tid / NCH;
+    chunk0 = (tid % NCH) ^ swz(row0);
   }
+  __device__ __forceinline__ int chunk(int i) const { return chunk0 ^ swz(i * STEP); }
   // LDS bytes of this wave's share of step i
   __device__ __forceinline__ uint32_t lds(const char* tile, int i) const {
-    return uniform(lds_offset(tile)) + i * THREADS * 16 + uniform(threadIdx.x >> 6) * 1024;
+    return uniform(lds_offset(tile)) + i * THREADS * 16 + uniform(tid >> 6) * 1024;
   }
 
   // Rows first .. of an array (row `first` at base), none past row `last` of the
   // tile (that row is repeated: what is past the end is masked).  Rows 16-byte
-  // aligned, a multiple of 8 wide, ROWS * sr below 2^31.
+  // aligned, a multiple of 8 wide, ROWS * sr below 2^31.  Every wave issues N
+  // copies (each row of a wave's share has a lane with a column).
   __device__ __forceinline__ void wide(char* tile, const char* base, uint32_t sr, int last, int width) const {
-    if (chunk * 8 >= width) return;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      copy16(base, (uint32_t)min(row0 + i * STEP, last) * sr + chunk * 16, lds(tile, i));
+      if (chunk(i) * 8 < width)
+        copy16(base, (uint32_t)min(row0 + i * STEP, last) * sr + chunk(i) * 16, lds(tile, i));
   }
-  // Rows anywhere: row(i) is the address of the thread's i-th row, NULL for a row
-  // that reads as NaN.
+  // The same from row addresses: row(i) is that of the thread's i-th row.
   template <typename Row>
   __device__ __forceinline__ void wide_rows(char* tile, int width, Row row) const {
-    if (chunk * 8 >= width) return;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const char* src = row(i);
-      if (src)
-        copy16(src + chunk * 16, lds(tile, i));
-      else
-        *reinterpret_cast<uint4*>(tile + (i * THREADS + threadIdx.x) * 16) =
-            uint4{kNanPair, kNanPair, kNanPair, kNanPair};
+      if (chunk(i) * 8 < width) copy16(src + chunk(i) * 16, lds(tile, i));
     }
   }
   // Element by element (any alignment and width).
@@ -260,11 +264,11 @@ struct TileCopy {
 #pragma unroll 1
     for (int i = 0; i < N; ++i) {
       const char* src = row(i);
+      const int c = chunk(i) * 8;
       uint32_t x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        x[e] = chunk * 8 + e >= width ? 0u : src ? reinterpret_cast<const uint16_t*>(src)[chunk * 8 + e] : 0x7fffu;
-      *reinterpret_cast<uint4*>(tile + (i * THREADS + threadIdx.x) * 16) =
+      for (int e = 0; e < 8; ++e) x[e] = c + e < width ? reinterpret_cast<const uint16_t*>(src)[c + e] : 0u;
+      *reinterpret_cast<uint4*>(tile + (i * THREADS + tid) * 16) =
           uint4{x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
     }
   }
@@ -360,12 +364,12 @@ __device__ __forceinline__ void contract(const char* tile, const TileLane<DP>& l
 // are then found apart (a rare path that keeps to a few registers).  Returns
 // whether the thread found any.
 template <typename T, int DP, int ROWS, int THREADS>
-__device__ __forceinline__ bool clean_tile(char* tile) {
+__device__ __forceinline__ bool clean_tile(char* tile, int tid) {
   constexpr uint32_t e = exponent_bits<T>();
   bool any = false;
 #pragma unroll
   for (int it = 0; it < ROWS * DP / 8 / THREADS; ++it) {
-    uint4* p = reinterpret_cast<uint4*>(tile + (it * THREADS + threadIdx.x) * 16);
+    uint4* p = reinterpret_cast<uint4*>(tile + (it * THREADS + tid) * 16);
     const uint4 x = *p;
     if (not_finite<T>(x)) {
       auto fix = [](uint32_t y) {
@@ -377,9 +381,6 @@ __device__ __forceinline__ bool clean_tile(char* tile) {
   }
   return any;
 }
-
-// Every copy of this wave's threads has landed (not yet those of other waves).
-__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // ------------------------------------------------------------- 16-bit output
 

@@ -276,7 +276,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
   // the stream: tiles of rows [r_lo, r_hi), once for every query head (KV)
   const int heads = KV ? s.G : 1, h0 = KV ? head * s.G : head / s.G;
   const int steps = r_hi > r_lo ? (r_hi - r_lo + BR - 1) / BR : 0;
-  const TileCopy<DP, BR, 64 * NW> tc;
+  const TileCopy<DP, BR, 64 * NW> tc(tid);
   auto issue = [&](int h, int row0, int stage) {
     char* t = smem + stage * 2 * TILE;
     const char* xb = X.p + b * X.sb + (int64_t)x0 * X.sr + (h0 + h) * X.sh;
@@ -305,12 +305,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
   for (int h = 0; h < heads; ++h)
     for (int st = 0; st < steps; ++st, stage ^= 1) {
       ++it;
+      copies_left<0>();
       const int row0 = r_lo + st * BR;
       const bool bordered = row0 + BR > all_hi || row0 < all_lo;
       if (bordered) {
-        copies_done();
         char* t = smem + stage * 2 * TILE;
-        if (clean_tile<T, DP, BR, 64 * NW>(t) | clean_tile<T, DP, BR, 64 * NW>(t + TILE)) mark[it & 3] = it;
+        if (clean_tile<T, DP, BR, 64 * NW>(t, tid) | clean_tile<T, DP, BR, 64 * NW>(t + TILE, tid)) mark[it & 3] = it;
       }
       tile_barrier();
       if (st + 1 < steps)

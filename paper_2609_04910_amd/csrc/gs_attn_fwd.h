@@ -5,9 +5,11 @@
 // a running offset o_m of the exponent (log2 units), and where a row's largest
 // exponent outgrows it the sums so far are scaled by exp2(old - new).
 //
-// A workgroup of NW waves streams 64-key (DP = 256: 32-key) tiles of K and V
-// through a two-stage LDS ring, one barrier a tile; wave w owns 16*NQ rows whose
-// query operands and output sums stay in registers.
+// k_attn_fwd: a workgroup of NW waves streams 64-key (DP = 256: 32-key) tiles of K
+// and V through an LDS ring, one barrier a tile; wave w owns 16*NQ rows whose query
+// operands and output sums stay in registers.  Bound by the matrix cores.
+// k_attn_rows: the same for few rows, bound by reading K and V.
+// Both can work on a part of a row's keys; k_attn_join then joins the parts.
 #pragma once
 
 #include "gs_attn.h"
@@ -35,6 +37,9 @@ struct AttnFwdArgs {
   int32_t heads;           // heads of the grid, all sequences of a dense call together
   int32_t neg;             // scale < 0: queries enter negated
   float c;                 // |scale| log2 e
+  int32_t splits;          // parts that a row's keys are cut into (1: results are written at once)
+  float* part_o;           // splits x rows x query heads x C: sums of weights times values
+  float* part_z;           // splits x rows x query heads x 2: offset and sum of weights
 };
 
 // Weights lie below 2^15 relative to the offset, the largest of a row between
@@ -45,21 +50,46 @@ constexpr float kOffsetBelow = 7.0f;
 constexpr float kOffsetLimit = 15.0f;
 constexpr float kNoOffset = -3.0e38f;
 
-// Page number of key j of sequence b, and the address of the key's row in a page;
-// NULL for a number outside the cache.
-__device__ __forceinline__ int page_of(const AttnPages& pg, int b, int j) {
-  const int pi = pg.shift >= 0 ? j >> pg.shift : (int)((uint32_t)j / (uint32_t)pg.size);
-  return pg.table[(int64_t)b * pg.width + pi];
+__device__ __forceinline__ int page_index(const AttnPages& pg, int j) {
+  return pg.shift >= 0 ? j >> pg.shift : (int)((uint32_t)j / (uint32_t)pg.size);
 }
 __device__ __forceinline__ const char* page_row(const AttnPages& pg, const char* base, int64_t page_stride, int64_t sr,
                                                 int page, int j) {
   const int off = pg.shift >= 0 ? j & (pg.size - 1) : (int)((uint32_t)j % (uint32_t)pg.size);
-  if ((uint32_t)page >= (uint32_t)pg.pages) return nullptr;
   return base + page * page_stride + off * sr;
 }
 
+// The part of a sequence's page table that a stretch of keys needs, in LDS: waiting
+// for a page number from memory between a tile's copies would wait for the copies
+// too.  Numbers outside the cache become -1, and their rows are read from page 0
+// (the scores of such keys are set to NaN).
+constexpr int kSlice = 2048;  // page numbers; a stretch is at most kSlice - 2 pages long
+struct PageSlice {
+  const int32_t* e;
+  int first;
+  bool bad;  // whether a number lies outside the cache
+  // Keys [key0, key1) of sequence b; a barrier of the workgroup.
+  __device__ __forceinline__ void load(const AttnPages& pg, int32_t* lds, int b, int key0, int key1, int threads) {
+    e = lds;
+    first = page_index(pg, key0);
+    const int n = page_index(pg, key1 - 1) - first + 1;
+    bool out = false;
+    for (int i = threadIdx.x; i < n; i += threads) {
+      const int p = pg.table[(int64_t)b * pg.width + first + i];
+      const bool ok = (uint32_t)p < (uint32_t)pg.pages;
+      lds[i] = ok ? p : -1;
+      out |= !ok;
+    }
+    bad = __syncthreads_or(out);
+  }
+  __device__ __forceinline__ int number(const AttnPages& pg, int j) const { return e[page_index(pg, j) - first]; }
+};
+
 template <int DP>
 constexpr int attn_keys() { return DP == 256 ? 32 : 64; }
+
+template <int DP>
+constexpr int attn_stages() { return 2; }
 
 // Query operand: columns 32c + 8g .. +7 of one row, zero past the width.
 template <typename T>
@@ -100,9 +130,14 @@ __device__ __forceinline__ void found_infinities(const AttnFwdArgs& a, const cha
 #pragma unroll
       for (int z = 0; z < 8; ++z) {
         const int j = min(key0 + 32 * h + 16 * (z >> 2) + 4 * g + (z & 3), kn - 1), c = 16 * ct + (lane & 15);
-        const char* p = PAGED ? page_row(a.pg, vb, a.pg.page_stride_v, a.v.sr, page_of(a.pg, b, j), j)
-                              : vb + (int64_t)j * a.v.sr;
-        const uint32_t x = p && c < a.s.C ? reinterpret_cast<const uint16_t*>(p)[c] : 0u;
+        const char* p;
+        if (PAGED) {
+          const int page = a.pg.table[(int64_t)b * a.pg.width + page_index(a.pg, j)];
+          p = page_row(a.pg, vb, a.pg.page_stride_v, a.v.sr, (uint32_t)page < (uint32_t)a.pg.pages ? page : 0, j);
+        } else {
+          p = vb + (int64_t)j * a.v.sr;
+        }
+        const uint32_t x = c < a.s.C ? reinterpret_cast<const uint16_t*>(p)[c] : 0u;
         u[z] = (x & e) == e && x != (e | 0x8000u) ? one : 0u;
         d[z] = (x & e) == e && x != e ? one : 0u;
       }
@@ -132,25 +167,45 @@ __device__ __forceinline__ void found_infinities(const AttnFwdArgs& a, const cha
   }
 }
 
-template <typename T, int DP, int NQ, int NW, bool PAGED, bool WIDE>
-__global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
-  constexpr int BK = attn_keys<DP>(), NC = DP / 32, NO = DP / 16, TILE = BK * DP * 2, ROWS = 16 * NQ * NW;
-  __shared__ __align__(1024) char smem[4 * TILE];
-  __shared__ int mark[4];
-  // infinities that reach the lane's results: bit 4 ct + r of its column tile n
-  constexpr int NB = (NO * 4 + 31) / 32;
-  __shared__ uint32_t inf_bits[64 * NW][2 * NQ * NB];
-  const AttnShape& s = a.s;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, g = lane >> 4;
+// Adds to the sums of column tile n, rows 4 ct .. of the lane's results, the
+// infinities that reach them.
+template <int NB, int NB2>
+__device__ __forceinline__ void add_infinities(const uint32_t (&bits)[NB2], int n, int ct, floatx4& y) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t bit = 1u << ((4 * ct + e) & 31);
+    if (bits[2 * n * NB + ct / 8] & bit) y[e] += __builtin_inff();
+    if (bits[(2 * n + 1) * NB + ct / 8] & bit) y[e] -= __builtin_inff();
+  }
+}
 
-  int tile, head, b;
-  block_place(blockIdx.x, a.heads, tile, head);
+// What a workgroup works on: a tile of rows of one sequence and key head, and a
+// stretch of its keys.
+struct AttnJob {
+  int b, kvh, head;    // head: the first of the `per` query heads of the rows, over per
+  AttnSeq sq;
+  int rows, limit;     // rows of the sequence (token-major, then its query heads), and rows that the call owns
+  int r0;              // first row of the tile
+  int part;            // which split
+};
+
+// Returns whether there is anything to do (rows of no sequence are handled here).
+template <int ROWS, bool PAGED>
+__device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
+  const AttnShape& s = a.s;
+  int id = blockIdx.x;
+  w.part = 0;
+  if (a.splits > 1) {
+    w.part = id % a.splits;
+    id /= a.splits;
+  }
+  int tile, head;
+  block_place(id, a.heads, tile, head);
   if (s.packed) {
     const int slot = a.tiles - 1 - tile;
-    b = packed_tile(s.q_index, s.B, s.M, a.per, ROWS, slot, tile);
-    if (b == kNoRow) {  // slots past the last tile: rows of no sequence
-      if (s.zero_rest) {
+    w.b = packed_tile(s.q_index, s.B, s.M, a.per, ROWS, slot, tile);
+    if (w.b == kNoRow) {  // slots past the last tile: rows of no sequence
+      if (s.zero_rest && w.part == 0) {
         const int part = slot - tile, parts = a.tiles - tile;
         const int end = s.B > 0 ? clampi(s.q_index[s.B], 0, s.M) : 0;
         for (int h = head * a.per; h < (head + 1) * a.per; ++h) {
@@ -163,94 +218,232 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
               if (threadIdx.x == 0) a.lse[h * a.lse_sh + r] = -__builtin_inff();
         }
       }
-      return;
+      return false;
     }
   } else {
     const int per_seq = a.heads / s.B;
-    b = head / per_seq;
-    head -= b * per_seq;
+    w.b = head / per_seq;
+    head -= w.b * per_seq;
     tile = a.tiles - 1 - tile;  // the tiles that see most keys first
   }
-  const int kvh = a.per > 1 ? head : head / s.G;
-  AttnSeq sq;
+  w.head = head;
+  w.kvh = a.per > 1 ? head : head / s.G;
   if (PAGED) {
     if (s.packed)
-      seq_side(s.q_index, 1, b, s.M, sq.q0, sq.qn);
+      seq_side(s.q_index, 1, w.b, s.M, w.sq.q0, w.sq.qn);
     else
-      sq.q0 = 0, sq.qn = s.M;
-    sq.k0 = 0;
-    sq.kn = clampi(a.pg.lens[b], 0, (int)min((int64_t)a.pg.width * a.pg.size, (int64_t)0x3fffffff));
-    sq.q0 = uniform(sq.q0), sq.qn = uniform(sq.qn), sq.kn = uniform(sq.kn);
+      w.sq.q0 = 0, w.sq.qn = s.M;
+    w.sq.q0 = uniform(w.sq.q0), w.sq.qn = uniform(w.sq.qn);
+    w.sq.k0 = 0;
+    // a cache without pages holds no keys
+    const int64_t room = a.pg.pages > 0 ? (int64_t)a.pg.width * a.pg.size : 0;
+    w.sq.kn = uniform(clampi(a.pg.lens[w.b], 0, (int)min(room, (int64_t)0x3fffffff)));
   } else {
-    sq = seq_of(s, b);
+    w.sq = seq_of(s, w.b);
   }
-  const int ahead = sq.kn - sq.qn;
-  const int rows = sq.qn * a.per;          // rows of this head group
-  const int limit = s.packed ? rows : s.M * a.per;  // and rows that the call owns
-  const int r0 = tile * ROWS;
-  if (r0 >= limit) return;
+  w.rows = w.sq.qn * a.per;
+  w.limit = s.packed ? w.rows : s.M * a.per;
+  w.r0 = tile * ROWS;
+  return w.r0 < w.limit;
+}
 
-  // the wave's rows: token and head of the lane's column in each of its tiles;
-  // rows past the end repeat the last one (nothing of them is written)
-  const int wr0 = r0 + wave * 16 * NQ;
-  int lo[NQ], hi[NQ];
-  uint4 qo[NQ][NC];
+// Keys that the rows [first, last] see: all of [in_lo, in_hi), none outside [lo, hi).
+struct KeyRange {
+  int lo = 0, hi = 0, in_lo = 0, in_hi = 0;
+};
+__device__ __forceinline__ KeyRange keys_of_rows(const AttnFwdArgs& a, const AttnJob& w, int first, int last) {
+  KeyRange r;
+  if (first >= w.rows) return r;
+  const int ahead = w.sq.kn - w.sq.qn;
+  query_range(a.s, first / a.per, ahead, w.sq.kn, r.lo, r.in_hi);
+  query_range(a.s, min(last, w.rows - 1) / a.per, ahead, w.sq.kn, r.in_lo, r.hi);
+  return r;
+}
+
+// This workgroup's part of the keys [lo, hi): cut into `splits` parts of whole
+// tiles, no part shorter than 256 keys.
+__device__ __forceinline__ void split_keys(const AttnFwdArgs& a, const AttnJob& w, int tile, int& lo, int& hi) {
+  lo = lo / tile * tile;
+  if (a.splits == 1) return;
+  int each = (hi - lo + a.splits - 1) / a.splits;
+  each = (max(each, 256) + tile - 1) / tile * tile;
+  const int64_t first = lo + (int64_t)w.part * each;
+  hi = first < hi ? (int)min(first + each, (int64_t)hi) : lo;
+  lo = first < hi ? (int)first : lo;
+}
+
+// A wave's rows: NQ tiles of 16, row 16 n + l%16 in the lane's column of tile n.
+template <typename T, int DP, int NQ>
+struct AttnRows {
+  static constexpr int NC = DP / 32, NO = DP / 16;
+  int lo[NQ], hi[NQ];      // keys that the row sees
+  uint4 q[NQ][NC];
+  floatx4 o[NO][NQ];       // sums of weights times values
+  float off[NQ], sum[NQ];  // offset of the exponents, sum of the weights in this lane
+
+  // Rows wr0 ..; rows past the end repeat the last one (nothing of them is written).
+  __device__ __forceinline__ void start(const AttnFwdArgs& a, const AttnJob& w, int wr0) {
+    const int col = threadIdx.x & 15;
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int r = min(wr0 + 16 * n + col, rows - 1);
-    const int token = a.per > 1 ? r / a.per : r;
-    const int h = a.per > 1 ? head * a.per + (r - token * a.per) : head;
-    lo[n] = hi[n] = 0;
-    if (rows > 0) {
-      query_range(s, token, ahead, sq.kn, lo[n], hi[n]);
-      const char* p = a.q.p + b * a.q.sb + (int64_t)(sq.q0 + token) * a.q.sr + h * a.q.sh;
+    for (int n = 0; n < NQ; ++n) {
+      const int r = min(wr0 + 16 * n + col, w.rows - 1);
+      const int token = a.per > 1 ? r / a.per : r;
+      const int h = a.per > 1 ? w.head * a.per + (r - token * a.per) : w.head;
+      lo[n] = hi[n] = 0;
+      off[n] = kNoOffset;
+      sum[n] = 0.0f;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) qo[n][c] = column_operand<T>(p, a.q.vec, s.D, c, a.neg);
+      for (int ct = 0; ct < NO; ++ct) o[ct][n] = floatx4{0, 0, 0, 0};
+      if (w.rows > 0) {
+        query_range(a.s, token, w.sq.kn - w.sq.qn, w.sq.kn, lo[n], hi[n]);
+        const char* p = a.q.p + w.b * a.q.sb + (int64_t)(w.sq.q0 + token) * a.q.sr + h * a.q.sh;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) q[n][c] = column_operand<T>(p, a.q.vec, a.s.D, c, a.neg);
+      }
     }
   }
-  // key ranges of the workgroup and of the wave (token ranges are monotone)
-  int k_lo = 0, k_hi = 0, w_lo = 0, w_hi = 0, in_lo = 0, in_hi = 0;
-  int all_lo = 0, all_hi = 0;  // keys that every row of the workgroup sees
-  if (rows > 0 && r0 < rows) {
-    query_range(s, r0 / a.per, ahead, sq.kn, k_lo, all_hi);
-    query_range(s, (min(r0 + ROWS, rows) - 1) / a.per, ahead, sq.kn, all_lo, k_hi);
-    const int f = min(wr0, rows - 1) / a.per, l = min(wr0 + 16 * NQ - 1, rows - 1) / a.per;
-    query_range(s, f, ahead, sq.kn, w_lo, in_hi);
-    query_range(s, l, ahead, sq.kn, in_lo, w_hi);
-    if (wr0 >= rows) w_hi = w_lo = 0;
-  }
-  k_lo = k_lo / BK * BK;
 
-  floatx4 o[NO][NQ];
-  float off[NQ], sum[NQ];
+  // The 32 keys key0 .. of step h of a tile.  masked: some row does not see all
+  // of them; bad: some of them may lie on a page outside the cache.
+  __device__ __forceinline__ void attend(const AttnFwdArgs& a, const char* kt, const char* vt, const TileLane<DP>& ln,
+                                         int h, int key0, bool masked, const PageSlice* pages) {
+    const int g = (threadIdx.x & 63) >> 4;
+    floatx4 x[2][NQ];
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    off[n] = kNoOffset;
-    sum[n] = 0.0f;
+    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-    for (int ct = 0; ct < NO; ++ct) o[ct][n] = floatx4{0, 0, 0, 0};
+      for (int n = 0; n < NQ; ++n) x[t][n] = floatx4{0, 0, 0, 0};
+      scores<T, DP, NQ>(kt, ln, 2 * h + t, q, x[t]);
+    }
+    if (masked || (pages && pages->bad)) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = key0 + 16 * t + 4 * g + r;
+          const bool nan = pages && pages->bad && pages->number(a.pg, min(j, max_key)) < 0;
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) {
+            x[t][n][r] = nan ? __builtin_nanf("") : x[t][n][r];
+            x[t][n][r] = j >= lo[n] && j < hi[n] ? x[t][n][r] : -__builtin_inff();
+          }
+        }
+    }
+    uint4 w[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      float mx = x[0][n][0];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[t][n][r]);
+      if (__any(__builtin_fmaf(mx, a.c, -off[n]) > kOffsetLimit)) {
+        mx *= a.c;
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const bool grow = mx - off[n] > kOffsetLimit;
+        const float next = grow ? mx - kOffsetBelow : off[n];
+        const float by = grow ? __builtin_amdgcn_exp2f(off[n] - next) : 1.0f;
+        off[n] = next;
+        sum[n] *= by;
+#pragma unroll
+        for (int ct = 0; ct < NO; ++ct) o[ct][n] *= by;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[t][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][n][r], a.c, -off[n]));
+          sum[n] += x[t][n][r];
+        }
+      // weights rounded to the values' type (the matrix cores take nothing
+      // wider): at most 2^-9 (bf16) or 2^-12 (fp16) of each; the sum of weights
+      // is of the unrounded ones
+      w[n] = uint4{pack2<T>(x[0][n][0], x[0][n][1]), pack2<T>(x[0][n][2], x[0][n][3]),
+                   pack2<T>(x[1][n][0], x[1][n][1]), pack2<T>(x[1][n][2], x[1][n][3])};
+    }
+    contract<T, DP>(vt, ln, h, w, o);
   }
+  int max_key;  // the last key whose page number is at hand
+};
+
+// Results of columns c .. c + 3 of row r (o / sum of weights z, offset off; first:
+// the thread that writes the row's own numbers): to the caller's arrays, or as
+// part of a row whose keys are split.
+template <typename T>
+__device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w, int r, int c, floatx4 o, float off,
+                                          float z, bool first) {
+  const AttnShape& s = a.s;
+  if (r >= w.limit) return;
+  const bool rest = r >= w.rows;
+  if (rest && (!s.zero_rest || a.splits > 1)) return;  // (parts: k_attn_join sees to them)
+  const int token = a.per > 1 ? r / a.per : r;
+  const int h = a.per > 1 ? w.head * a.per + (r - token * a.per) : w.head;
+  const int64_t row = w.sq.q0 + token;
+  if (a.splits > 1) {
+    const int64_t at = ((w.part * (int64_t)(s.packed ? 1 : s.B) + (s.packed ? 0 : w.b)) * s.M + row) * s.Hq + h;
+    float* p = a.part_o + at * s.C + c;
+    if ((s.C & 3) == 0) {
+      if (c < s.C) *reinterpret_cast<floatx4*>(p) = o;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < s.C) p[e] = o[e];
+    }
+    if (first) a.part_z[2 * at] = off, a.part_z[2 * at + 1] = z;
+    return;
+  }
+  const bool empty = rest || z == 0.0f;
+  const float inv = 1.0f / z;
+  floatx4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : o[e] * inv;
+  if (!rest || (s.zero_rest & kRestOut)) {
+    store4<T>(a.out.p + w.b * a.out.sb + row * a.out.sr + h * a.out.sh, c, s.C, a.out.vec, y[0], y[1], y[2], y[3]);
+    if (a.low.p)
+      store4<T>(a.low.p + w.b * a.low.sb + row * a.low.sr + h * a.low.sh, c, s.C, a.low.vec, left<T>(y[0]),
+                left<T>(y[1]), left<T>(y[2]), left<T>(y[3]));
+  }
+  if (first && a.lse && (!rest || (s.zero_rest & kRestLse)))
+    a.lse[w.b * a.lse_sb + h * a.lse_sh + row] = empty ? -__builtin_inff() : (off + __builtin_amdgcn_logf(z)) * kLn2;
+}
+
+template <typename T, int DP, int NQ, int NW, bool PAGED, bool WIDE>
+__global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
+  constexpr int BK = attn_keys<DP>(), NS = attn_stages<DP>(), NO = DP / 16, TILE = BK * DP * 2, ROWS = 16 * NQ * NW;
+  constexpr int NB = (NO * 4 + 31) / 32;
+  __shared__ __align__(1024) char smem[NS * 2 * TILE];
+  __shared__ int mark[4];
+  // infinities that reach the lane's results: bit 4 ct + r of its column tile n
+  __shared__ uint32_t inf_bits[64 * NW][2 * NQ * NB];
+  __shared__ int32_t slice[PAGED ? kSlice : 1];
+  const AttnShape& s = a.s;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+
+  AttnJob job;
+  if (!attn_job<ROWS, PAGED>(a, job)) return;
+  const int kn = job.sq.kn, wr0 = job.r0 + wave * 16 * NQ;
+  AttnRows<T, DP, NQ> rows;
+  rows.start(a, job, wr0);
+  const KeyRange all = keys_of_rows(a, job, job.r0, job.r0 + ROWS - 1);
+  const KeyRange mine = keys_of_rows(a, job, wr0, wr0 + 16 * NQ - 1);
+  int k_lo = all.lo, k_hi = all.hi;
+  split_keys(a, job, BK, k_lo, k_hi);
 
   const TileLane<DP> ln;
-  const char* kb = a.k.p + (PAGED ? 0 : b * a.k.sb + (int64_t)sq.k0 * a.k.sr) + kvh * a.k.sh;
-  const char* vb = a.v.p + (PAGED ? 0 : b * a.v.sb + (int64_t)sq.k0 * a.v.sr) + kvh * a.v.sh;
+  const char* kb = a.k.p + (PAGED ? 0 : job.b * a.k.sb + (int64_t)job.sq.k0 * a.k.sr) + job.kvh * a.k.sh;
+  const char* vb = a.v.p + (PAGED ? 0 : job.b * a.v.sb + (int64_t)job.sq.k0 * a.v.sr) + job.kvh * a.v.sh;
+  const TileCopy<DP, BK, 64 * NW> tc(threadIdx.x);
+  PageSlice pages;
   // Copies of a tile into a stage; rows past the last key repeat it (they are
-  // masked, and stay in the array).  Page numbers are read a tile ahead: waiting
-  // for them between a tile's copies would wait for the copies too.
-  const TileCopy<DP, BK, 64 * NW> tc;
-  int pages[PAGED ? TileCopy<DP, BK, 64 * NW>::N : 1];
-  auto key_of = [&](int key0, int i) { return min(key0 + tc.row0 + i * tc.STEP, sq.kn - 1); };
-  auto read_pages = [&](int key0) {
-    if constexpr (PAGED) {
-#pragma unroll
-      for (int i = 0; i < tc.N; ++i) pages[i] = page_of(a.pg, b, key_of(key0, i));
-    }
-  };
-  auto issue = [&](int key0, int stage) {
+  // masked, and stay in the array).
+  auto issue = [&](int key0, int stage, int end) {
     char* t = smem + stage * 2 * TILE;
+    auto key_of = [&](int i) { return min(key0 + tc.row0 + i * tc.STEP, (PAGED ? end : kn) - 1); };
     if constexpr (PAGED) {
-      auto krow = [&](int i) { return page_row(a.pg, kb, a.pg.page_stride_k, a.k.sr, pages[i], key_of(key0, i)); };
-      auto vrow = [&](int i) { return page_row(a.pg, vb, a.pg.page_stride_v, a.v.sr, pages[i], key_of(key0, i)); };
+      auto page = [&](int i) { return max(pages.number(a.pg, key_of(i)), 0); };
+      auto krow = [&](int i) { return page_row(a.pg, kb, a.pg.page_stride_k, a.k.sr, page(i), key_of(i)); };
+      auto vrow = [&](int i) { return page_row(a.pg, vb, a.pg.page_stride_v, a.v.sr, page(i), key_of(i)); };
       if constexpr (WIDE) {
         tc.wide_rows(t, s.D, krow);
         tc.wide_rows(t + TILE, s.C, vrow);
@@ -258,135 +451,251 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
         tc.narrow_rows(t, s.D, krow);
         tc.narrow_rows(t + TILE, s.C, vrow);
       }
-      if (key0 + BK < k_hi) read_pages(key0 + BK);
     } else if constexpr (WIDE) {
-      tc.wide(t, kb + (int64_t)key0 * a.k.sr, (uint32_t)a.k.sr, sq.kn - 1 - key0, s.D);
-      tc.wide(t + TILE, vb + (int64_t)key0 * a.v.sr, (uint32_t)a.v.sr, sq.kn - 1 - key0, s.C);
+      tc.wide(t, kb + (int64_t)key0 * a.k.sr, (uint32_t)a.k.sr, kn - 1 - key0, s.D);
+      tc.wide(t + TILE, vb + (int64_t)key0 * a.v.sr, (uint32_t)a.v.sr, kn - 1 - key0, s.C);
     } else {
-      tc.narrow_rows(t, s.D, [&](int i) { return kb + (int64_t)key_of(key0, i) * a.k.sr; });
-      tc.narrow_rows(t + TILE, s.C, [&](int i) { return vb + (int64_t)key_of(key0, i) * a.v.sr; });
+      tc.narrow_rows(t, s.D, [&](int i) { return kb + (int64_t)key_of(i) * a.k.sr; });
+      tc.narrow_rows(t + TILE, s.C, [&](int i) { return vb + (int64_t)key_of(i) * a.v.sr; });
     }
   };
 
   if (s.D < DP || s.C < DP) {
-    clear_tiles<64 * NW>(smem, 4 * TILE);
+    clear_tiles<64 * NW>(smem, NS * 2 * TILE);
     __syncthreads();
   }
   bool infinities = false;
-  if (k_lo < k_hi) {
-    read_pages(k_lo);
-    issue(k_lo, 0);
-  }
-  int stage = 0;
-  for (int key0 = k_lo, it = 1; key0 < k_hi; key0 += BK, stage ^= 1, ++it) {
-    const bool bordered = key0 + BK > all_hi || key0 < all_lo;
-    if (bordered) {
-      copies_done();
-      if (clean_tile<T, DP, BK, 64 * NW>(smem + (stage * 2 + 1) * TILE)) mark[it & 3] = it;
+  int it = 0;
+  // keys in stretches whose page numbers fit in LDS (not paged: one stretch)
+  const int64_t most = PAGED ? max((int64_t)(kSlice - 2) * a.pg.size / BK * BK, (int64_t)BK) : (int64_t)1 << 31;
+  for (int from = k_lo; from < k_hi;) {
+    const int to = (int)min(from + most, (int64_t)k_hi);
+    if constexpr (PAGED) {
+      if (from > k_lo) __syncthreads();  // nobody reads the last stretch's numbers
+      pages.load(a.pg, slice, job.b, from, to, 64 * NW);
+      rows.max_key = to - 1;
     }
-    tile_barrier();  // this tile has landed, and nobody reads the other stage
-    if (key0 + BK < k_hi) issue(key0 + BK, stage ^ 1);
-    if (bordered && uniform(mark[it & 3]) == it) {
-      found_infinities<T, DP, BK, NQ, PAGED>(a, vb, b, sq.kn, key0, lo, hi, inf_bits[threadIdx.x], !infinities);
-      infinities = true;
+#pragma unroll
+    for (int k = 0; k < NS - 1; ++k)
+      if (from + k * BK < to) issue(from + k * BK, k, to);
+    int stage = 0;
+    for (int key0 = from; key0 < to; key0 += BK) {
+      ++it;
+      // this tile's copies are done; those of the NS - 2 next ones may be in flight
+      if (key0 + (NS - 2) * BK < to)
+        copies_left<(NS - 2) * 2 * TileCopy<DP, BK, 64 * NW>::N>();
+      else
+        copies_left<0>();
+      const bool bordered = key0 + BK > all.in_hi || key0 < all.in_lo;
+      if (bordered && clean_tile<T, DP, BK, 64 * NW>(smem + (stage * 2 + 1) * TILE, threadIdx.x)) mark[it & 3] = it;
+      tile_barrier();  // this tile has landed everywhere, and nobody reads the stage before it
+      if (key0 + (NS - 1) * BK < to) issue(key0 + (NS - 1) * BK, stage == 0 ? NS - 1 : stage - 1, to);
+      if (bordered && uniform(mark[it & 3]) == it) {
+        found_infinities<T, DP, BK, NQ, PAGED>(a, vb, job.b, kn, key0, rows.lo, rows.hi, inf_bits[threadIdx.x],
+                                               !infinities);
+        infinities = true;
+      }
+      if (key0 < mine.hi && key0 + BK > mine.lo) {
+        const char* kt = smem + stage * 2 * TILE;
+        const bool masked = key0 + BK > mine.in_hi || key0 < mine.in_lo;
+#pragma unroll
+        for (int h = 0; h < BK / 32; ++h)
+          rows.attend(a, kt, kt + TILE, ln, h, key0 + 32 * h, masked, PAGED ? &pages : nullptr);
+      }
+      stage = stage + 1 == NS ? 0 : stage + 1;
     }
-    if (key0 >= w_hi || key0 + BK <= w_lo) continue;
-    const char* kt = smem + stage * 2 * TILE;
-    const char* vt = kt + TILE;
-    const bool masked = key0 + BK > in_hi || key0 < in_lo;
-#pragma unroll
-    for (int h = 0; h < BK / 32; ++h) {
-      floatx4 x[2][NQ];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) x[t][n] = floatx4{0, 0, 0, 0};
-        scores<T, DP, NQ>(kt, ln, 2 * h + t, qo, x[t]);
-      }
-      if (masked) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int n = 0; n < NQ; ++n)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int j = key0 + 32 * h + 16 * t + 4 * g + r;
-              x[t][n][r] = j >= lo[n] && j < hi[n] ? x[t][n][r] : -__builtin_inff();
-            }
-      }
-      uint4 w[NQ];
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        float mx = x[0][n][0];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[t][n][r]);
-        if (__any(__builtin_fmaf(mx, a.c, -off[n]) > kOffsetLimit)) {
-          mx *= a.c;
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
-          const bool grow = mx - off[n] > kOffsetLimit;
-          const float next = grow ? mx - kOffsetBelow : off[n];
-          const float by = grow ? __builtin_amdgcn_exp2f(off[n] - next) : 1.0f;
-          off[n] = next;
-          sum[n] *= by;
-#pragma unroll
-          for (int ct = 0; ct < NO; ++ct) o[ct][n] *= by;
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            x[t][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][n][r], a.c, -off[n]));
-            sum[n] += x[t][n][r];
-          }
-        // weights rounded to the values' type (the matrix cores take nothing
-        // wider): at most 2^-9 (bf16) or 2^-12 (fp16) of each; the sum of weights
-        // is of the unrounded ones
-        w[n] = uint4{pack2<T>(x[0][n][0], x[0][n][1]), pack2<T>(x[0][n][2], x[0][n][3]),
-                     pack2<T>(x[1][n][0], x[1][n][1]), pack2<T>(x[1][n][2], x[1][n][3])};
-      }
-      contract<T, DP>(vt, ln, h, w, o);
-    }
+    from = to;
   }
 
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    const int r = wr0 + 16 * n + col;
-    float z = sum[n];
+    float z = rows.sum[n];
     z += __shfl_xor(z, 16);
     z += __shfl_xor(z, 32);
-    if (r >= limit || (r >= rows && !s.zero_rest)) continue;
-    const int tk = a.per > 1 ? r / a.per : r;
-    const int h = a.per > 1 ? head * a.per + (r - tk * a.per) : head;
-    if (r >= rows) z = 0.0f;
-    const bool empty = z == 0.0f;
-    const float inv = empty ? 0.0f : 1.0f / z;
-    char* p = a.out.p + b * a.out.sb + (int64_t)(sq.q0 + tk) * a.out.sr + h * a.out.sh;
-    char* pl = a.low.p ? a.low.p + b * a.low.sb + (int64_t)(sq.q0 + tk) * a.low.sr + h * a.low.sh : nullptr;
-    const bool rest = r >= rows;
 #pragma unroll
     for (int ct = 0; ct < NO; ++ct) {
-      if (rest && !(s.zero_rest & kRestOut)) break;
-      floatx4 y = o[ct][n];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t bit = 1u << ((4 * ct + e) & 31);
-        y[e] = empty ? 0.0f : y[e] * inv;
-        if (infinities) {
-          if (inf_bits[threadIdx.x][2 * n * NB + ct / 8] & bit) y[e] += __builtin_inff();
-          if (inf_bits[threadIdx.x][(2 * n + 1) * NB + ct / 8] & bit) y[e] -= __builtin_inff();
-        }
-      }
-      store4<T>(p, 16 * ct + 4 * g, s.C, a.out.vec, y[0], y[1], y[2], y[3]);
-      if (pl)
-        store4<T>(pl, 16 * ct + 4 * g, s.C, a.low.vec, left<T>(y[0]), left<T>(y[1]), left<T>(y[2]), left<T>(y[3]));
+      floatx4 y = rows.o[ct][n];
+      if (infinities) add_infinities<NB>(inf_bits[threadIdx.x], n, ct, y);
+      write_row<T>(a, job, wr0 + 16 * n + (lane & 15), 16 * ct + 4 * (lane >> 4), y, rows.off[n], z,
+                   ct == 0 && lane < 16);
     }
-    if (a.lse && g == 0 && (!rest || (s.zero_rest & kRestLse)))
-      a.lse[b * a.lse_sb + h * a.lse_sh + sq.q0 + tk] =
-          empty ? -__builtin_inff() : (off[n] + __builtin_amdgcn_logf(z)) * kLn2;
   }
+}
+
+// The same for few rows (16 NQ, for instance the query heads that share a key head,
+// of one new token): bound by reading the keys and values once, so the NW waves of a
+// workgroup share the rows and take 32-key tiles in turn, each through a ring of its
+// own (no barrier in the loop), and their sums are joined at the end.
+template <typename T, int DP, int NQ, int NW, bool PAGED, bool WIDE>
+__global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
+  constexpr int NO = DP / 16, TILE = 32 * DP * 2, ROWS = 16 * NQ, NB = (NO * 4 + 31) / 32, NT = 64 * NW;
+  constexpr int RING = NW * 2 * 2 * TILE, JOIN = NW * NQ * NO * 64 * 16;
+  __shared__ __align__(1024) char smem[RING > JOIN ? RING : JOIN];
+  __shared__ uint32_t inf_bits[NT][2 * NQ * NB];
+  __shared__ int32_t slice[PAGED ? kSlice : 1];
+  __shared__ float w_off[NW][ROWS], w_sum[NW][ROWS];
+  const AttnShape& s = a.s;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+
+  AttnJob job;
+  if (!attn_job<ROWS, PAGED>(a, job)) return;
+  const int kn = job.sq.kn;
+  AttnRows<T, DP, NQ> rows;
+  rows.start(a, job, job.r0);
+  const KeyRange all = keys_of_rows(a, job, job.r0, job.r0 + ROWS - 1);
+  int k_lo = all.lo, k_hi = all.hi;
+  split_keys(a, job, 32, k_lo, k_hi);
+
+  const TileLane<DP> ln;
+  const char* kb = a.k.p + (PAGED ? 0 : job.b * a.k.sb + (int64_t)job.sq.k0 * a.k.sr) + job.kvh * a.k.sh;
+  const char* vb = a.v.p + (PAGED ? 0 : job.b * a.v.sb + (int64_t)job.sq.k0 * a.v.sr) + job.kvh * a.v.sh;
+  const TileCopy<DP, 32, 64> tc(lane);
+  char* ring = smem + wave * 4 * TILE;
+  PageSlice pages;
+  auto issue = [&](int key0, int stage, int end) {
+    char* t = ring + stage * 2 * TILE;
+    auto key_of = [&](int i) { return min(key0 + tc.row0 + i * tc.STEP, (PAGED ? end : kn) - 1); };
+    if constexpr (PAGED) {
+      auto page = [&](int i) { return max(pages.number(a.pg, key_of(i)), 0); };
+      auto krow = [&](int i) { return page_row(a.pg, kb, a.pg.page_stride_k, a.k.sr, page(i), key_of(i)); };
+      auto vrow = [&](int i) { return page_row(a.pg, vb, a.pg.page_stride_v, a.v.sr, page(i), key_of(i)); };
+      if constexpr (WIDE) {
+        tc.wide_rows(t, s.D, krow);
+        tc.wide_rows(t + TILE, s.C, vrow);
+      } else {
+        tc.narrow_rows(t, s.D, krow);
+        tc.narrow_rows(t + TILE, s.C, vrow);
+      }
+    } else if constexpr (WIDE) {
+      tc.wide(t, kb + (int64_t)key0 * a.k.sr, (uint32_t)a.k.sr, kn - 1 - key0, s.D);
+      tc.wide(t + TILE, vb + (int64_t)key0 * a.v.sr, (uint32_t)a.v.sr, kn - 1 - key0, s.C);
+    } else {
+      tc.narrow_rows(t, s.D, [&](int i) { return kb + (int64_t)key_of(i) * a.k.sr; });
+      tc.narrow_rows(t + TILE, s.C, [&](int i) { return vb + (int64_t)key_of(i) * a.v.sr; });
+    }
+  };
+
+  if (s.D < DP || s.C < DP) {
+    clear_tiles<NT>(smem, RING);
+    __syncthreads();
+  }
+  bool infinities = false;
+  const int64_t most = PAGED ? max((int64_t)(kSlice - 2) * a.pg.size / 32 * 32, (int64_t)32) : (int64_t)1 << 31;
+  for (int from = k_lo; from < k_hi;) {
+    const int to = (int)min(from + most, (int64_t)k_hi);
+    if constexpr (PAGED) {
+      if (from > k_lo) __syncthreads();
+      pages.load(a.pg, slice, job.b, from, to, NT);
+      rows.max_key = to - 1;
+    }
+    const int step = 32 * NW;
+    if (from + 32 * wave < to) issue(from + 32 * wave, 0, to);
+    int stage = 0;
+    for (int key0 = from + 32 * wave; key0 < to; key0 += step, stage ^= 1) {
+      copies_left<0>();  // this tile has landed, and nothing reads the other stage
+      if (key0 + step < to) issue(key0 + step, stage ^ 1, to);
+      char* kt = ring + stage * 2 * TILE;
+      const bool masked = key0 + 32 > all.in_hi || key0 < all.in_lo;
+      if (masked && __any(clean_tile<T, DP, 32, 64>(kt + TILE, lane))) {
+        found_infinities<T, DP, 32, NQ, PAGED>(a, vb, job.b, kn, key0, rows.lo, rows.hi, inf_bits[threadIdx.x],
+                                               !infinities);
+        infinities = true;
+      }
+      rows.attend(a, kt, kt + TILE, ln, 0, key0, masked, PAGED ? &pages : nullptr);
+    }
+    from = to;
+  }
+
+  // join the waves' sums at the largest of their offsets
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    float z = rows.sum[n];
+    z += __shfl_xor(z, 16);
+    z += __shfl_xor(z, 32);
+    if (lane < 16) w_off[wave][16 * n + lane] = rows.off[n], w_sum[wave][16 * n + lane] = z;
+  }
+  __syncthreads();  // also: every wave is done with its ring
+  floatx4* join = reinterpret_cast<floatx4*>(smem);
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    float top = kNoOffset;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, w_off[w][16 * n + (lane & 15)]);
+    const float by = __builtin_amdgcn_exp2f(rows.off[n] - top);
+#pragma unroll
+    for (int ct = 0; ct < NO; ++ct) {
+      floatx4 y = rows.o[ct][n] * by;
+      if (infinities) add_infinities<NB>(inf_bits[threadIdx.x], n, ct, y);
+      join[((wave * NQ + n) * NO + ct) * 64 + lane] = y;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < NQ * NO * 64; i += NT) {
+    const int l = i & 63, n = i / (NO * 64), ct = (i >> 6) % NO, r = 16 * n + (l & 15);
+    float top = kNoOffset, z = 0.0f;
+    floatx4 y{0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, w_off[w][r]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      z += w_sum[w][r] * __builtin_amdgcn_exp2f(w_off[w][r] - top);
+      y += join[w * NQ * NO * 64 + i];
+    }
+    write_row<T>(a, job, job.r0 + r, 16 * ct + 4 * (l >> 4), y, top, z, ct == 0 && l < 16);
+  }
+}
+
+// Joins the parts of rows whose keys were split: one wave a row and query head.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
+  const AttnShape& s = a.s;
+  const int lane = threadIdx.x & 63;
+  const int64_t units = (int64_t)(s.packed ? 1 : s.B) * s.M * s.Hq;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (unit >= units) return;
+  const int h = (int)(unit % s.Hq);
+  const int64_t at = unit / s.Hq;
+  const int b = s.packed ? 0 : (int)(at / s.M);
+  const int64_t row = at - (int64_t)b * s.M;
+  char* out = a.out.p + b * a.out.sb + row * a.out.sr + h * a.out.sh;
+  char* low = a.low.p ? a.low.p + b * a.low.sb + row * a.low.sr + h * a.low.sh : nullptr;
+  float* lse = a.lse ? a.lse + b * a.lse_sb + h * a.lse_sh + row : nullptr;
+  if (s.packed) {
+    // rows of no sequence are written, or left, by the main kernel
+    if (row < clampi(s.q_index[0], 0, s.M) || row >= clampi(s.q_index[s.B], 0, s.M)) return;
+  } else if (s.q_index && row >= clampi(s.q_index[b], 0, s.M)) {
+    if (s.zero_rest & kRestOut)
+      for (int c = lane; c < s.C; c += 64) {
+        reinterpret_cast<uint16_t*>(out)[c] = 0;
+        if (low) reinterpret_cast<uint16_t*>(low)[c] = 0;
+      }
+    if (lse && lane == 0 && (s.zero_rest & kRestLse)) *lse = -__builtin_inff();
+    return;
+  }
+  float top = kNoOffset, z = 0.0f;
+  for (int p = 0; p < a.splits; ++p) top = fmaxf(top, a.part_z[2 * (p * units + unit)]);
+  for (int p = 0; p < a.splits; ++p)
+    z += a.part_z[2 * (p * units + unit) + 1] * __builtin_amdgcn_exp2f(a.part_z[2 * (p * units + unit)] - top);
+  const bool empty = z == 0.0f;
+  const float inv = 1.0f / z;
+  for (int c = lane * 4; c < s.C; c += 256) {
+    floatx4 y{0, 0, 0, 0};
+    for (int p = 0; p < a.splits; ++p) {
+      const float w = __builtin_amdgcn_exp2f(a.part_z[2 * (p * units + unit)] - top);
+      const float* o = a.part_o + (p * units + unit) * s.C + c;
+      if ((s.C & 3) == 0) {
+        y += *reinterpret_cast<const floatx4*>(o) * w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] += c + e < s.C ? o[e] * w : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : y[e] * inv;
+    store4<T>(out, c, s.C, a.out.vec, y[0], y[1], y[2], y[3]);
+    if (low) store4<T>(low, c, s.C, a.low.vec, left<T>(y[0]), left<T>(y[1]), left<T>(y[2]), left<T>(y[3]));
+  }
+  if (lse && lane == 0) *lse = empty ? -__builtin_inff() : (top + __builtin_amdgcn_logf(z)) * kLn2;
 }
 
 }  // namespace gs

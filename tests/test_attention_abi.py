@@ -119,6 +119,10 @@ def test_workspace_sizes():
     assert f(at._ref(problem()), 0, 0, 0) == 0 and f(at._ref(problem(D=0)), 1, 1, 1) == 0 and f(None, 1, 1, 1) == 0
     assert at.load().gs_attention_paged_workspace_size(None, None) == 0
     assert at.load().gs_attention_fwd_workspace_size(None) == 0
+    long = problem(B=1, M=1, N=100000)
+    need = at.load().gs_attention_fwd_workspace_size(at._ref(long))
+    assert need >= 2 * 4 * (32 + 2) * 4 and need < 1 << 24
+    assert fwd(long) == 6                                     # the parts of its rows need a workspace
 
 
 def cache(pages=6, size=16, width=3, k=None, v=None, table=FAKE + 12 * STEP, lens=FAKE + 13 * STEP, C=32):

@@ -64,6 +64,14 @@ SHAPES = [  # B, M, N, Hq, Hkv, D, C, causal, window
     (1, 140, 140, 2, 1, 256, 256, True, 0),
     (1, 70, 40, 2, 1, 200, 129, False, 0),
     (1, 90, 600, 8, 1, 128, 64, True, 0),
+    # few rows, or few workgroups: the keys are cut into parts
+    (1, 1, 5000, 8, 2, 128, 128, False, 0),
+    (2, 3, 3000, 4, 4, 64, 64, True, 0),
+    (1, 20, 4000, 2, 1, 64, 48, True, 900),
+    (1, 5, 2000, 3, 1, 33, 17, False, 0),
+    (1, 2, 1500, 2, 1, 256, 256, False, 0),
+    (1, 200, 3000, 1, 1, 128, 100, True, 0),
+    (1, 3000, 1100, 1, 1, 64, 64, True, 0),  # most rows see nothing
 ]
 
 
@@ -152,6 +160,48 @@ def test_packed_against_64_bits(at, case, dtype):
     assert not out[sum(rows):].any() and not dq[sum(rows):].any()
     assert not dk[sum(keys):].any() and not dv[sum(keys):].any()
     assert (lse[:, sum(rows):] == -math.inf).all()
+
+
+@pytest.mark.parametrize("M,N", [(6, 3000), (150, 3000)])
+def test_lengths_where_keys_are_cut_into_parts(at, M, N):
+    rows, keys = [M, 1, 0, 3], [N, 700, 900, 0]
+    q, k, v, g = make(22, 4, M, N, 2, 1, 64, 64, torch.bfloat16)
+    for t, n in ((q, rows), (k, keys), (v, keys)):
+        for b in range(4):
+            t[b, n[b]:] = float("nan")
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (rows, keys)]
+    assert at.attention_fwd_workspace_size(4, M, N, 2, 1, 64, 64) > 0
+    kw = dict(q_lens=lens[0], k_lens=lens[1], causal=True)
+    check_dense(at, q, k, v, g, rows=rows, keys=keys, **kw)
+    out, lse, low = torch.full_like(q, 7.0), torch.full((4, 2, M), 7.0, device="cuda"), torch.full_like(q, 7.0)
+    at.attention_fwd(q, k, v, out=out, lse=lse, low=low, **kw)
+    fresh, _ = at.attention_fwd(q, k, v, **kw)
+    for b in range(4):
+        assert (out[b, rows[b]:] == 7).all() and (low[b, rows[b]:] == 7).all() and (lse[b, :, rows[b]:] == 7).all()
+        assert torch.equal(out[b, :rows[b]], fresh[b, :rows[b]])
+        exact = ref.one(q[b, :rows[b]], k[b, :keys[b]], v[b, :keys[b]], 0.125, True)["out"][0]
+        assert (out[b, :rows[b]].cpu().double() - exact).norm() + 1e-9 >= \
+            (out[b, :rows[b]].cpu().double() + low[b, :rows[b]].cpu().double() - exact).norm()
+
+
+def test_packed_rows_of_few_keys_and_many(at):
+    gen = torch.Generator().manual_seed(23)
+    rows, keys = [3, 1, 0, 2], [4000, 9, 500, 1700]
+    q = normal(gen, (sum(rows) + 2, 4, 64), torch.float16)
+    k, v = (normal(gen, (sum(keys), 2, 64), torch.float16) for _ in range(2))
+    offs = [torch.tensor([sum(x[:i]) for i in range(5)], dtype=torch.int32, device="cuda") for x in (rows, keys)]
+    assert at.attention_fwd_workspace_size(4, 8, sum(keys), 4, 2, 64, 64, packed=True) > 0
+    kw = dict(q_offsets=offs[0], k_offsets=offs[1])
+    out, lse = at.attention_fwd(q, k, v, **kw)
+    mine = torch.full_like(out, 7.0)
+    at.attention_fwd(q, k, v, out=mine, **kw)
+    for b in range(4):
+        i, j = slice(sum(rows[:b]), sum(rows[:b + 1])), slice(sum(keys[:b]), sum(keys[:b + 1]))
+        r = ref.one(q[i], k[j], v[j], 0.125)
+        ref.check("out", out[i], *r["out"])
+        ref.check("lse", lse[:, i], *r["lse"])
+        assert torch.equal(mine[i], out[i])
+    assert not out[6:].any() and (lse[:, 6:] == -math.inf).all() and (mine[6:] == 7).all()
 
 
 def test_rows_of_no_sequence_in_the_callers_arrays_are_left(at):
