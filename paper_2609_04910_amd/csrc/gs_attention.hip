@@ -247,11 +247,11 @@ FwdPlan fwd_plan(const gs_attention_problem& p, bool paged, int64_t keys, void* 
   f.rows = !few ? attn_fwd_rows(DP) : shared <= 16 ? 16 : rows_most(DP);
   f.tiles = tiles_of(p, p.M * f.per, f.rows);
   f.heads = (f.per > 1 || G == 1 ? p.Hkv : p.Hq) * B;
-  // With few workgroups a row's keys are cut into parts, none shorter than 256:
-  // k_attn_rows up to 1024 workgroups, four a CU, so that sequences of unequal
-  // length even out; k_attn_fwd to 512, two a CU
-  const int64_t wgs = f.tiles * f.heads, want = few ? 1024 : 512;
-  f.splits = wgs > 0 ? std::max<int64_t>(1, std::min({want / wgs, keys / 256, (int64_t)64})) : 1;
+  // With few workgroups a row's keys are cut into parts
+  const int64_t wgs = f.tiles * f.heads, want = few ? 512 : 512, least = few ? 256 : 512;
+  f.splits = wgs > 0 && keys >= 2 * least
+                 ? std::max<int64_t>(1, std::min({want / wgs, keys / least, (int64_t)kMostParts}))
+                 : 1;
   f.grid = wgs * f.splits;
   if (f.splits > 1) {
     Carve c{static_cast<char*>(ws)};

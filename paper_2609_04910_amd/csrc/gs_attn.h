@@ -258,6 +258,18 @@ struct TileCopy {
       if (chunk(i) * 8 < width) copy16(src + chunk(i) * 16, lds(tile, i));
     }
   }
+  // The same where the RW rows of each of a wave's copies lie sr apart: base(i) is
+  // the address, the same in all lanes, of the first row of the wave's copy i, the
+  // tile's row wave_row + i * STEP.
+  static constexpr int RW = 64 / NCH;
+  __device__ __forceinline__ int wave_row() const { return uniform(tid >> 6) * RW; }
+  template <typename Base>
+  __device__ __forceinline__ void wide_bases(char* tile, int width, uint32_t sr, Base base) const {
+    const uint32_t row = (uint32_t)((tid & 63) / NCH) * sr;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (chunk(i) * 8 < width) copy16(base(i), row + chunk(i) * 16, lds(tile, i));
+  }
   // Element by element (any alignment and width).
   template <typename Row>
   __device__ __forceinline__ void narrow_rows(char* tile, int width, Row row) const {

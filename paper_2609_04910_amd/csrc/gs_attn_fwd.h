@@ -108,6 +108,41 @@ __device__ __forceinline__ uint4 column_operand(const char* row, int vec, int wi
   return x;
 }
 
+// Copies a tile of keys and values key0 .. from the pages; rows past key end - 1 are
+// others of the cache (they are masked, and cleaned).  Where a page holds a power
+// of two of at least 8 rows, the rows of a wave's copy lie in one page: its
+// address is then found once a copy, in scalar registers.
+template <bool WIDE, typename Copy>
+__device__ __forceinline__ void copy_pages(const AttnFwdArgs& a, const PageSlice& pages, const Copy& tc, char* kt,
+                                           char* vt, const char* kb, const char* vb, int key0, int end) {
+  const AttnPages& pg = a.pg;
+  if (WIDE && pg.shift >= 3) {
+    int page[Copy::N], off[Copy::N];
+#pragma unroll
+    for (int i = 0; i < Copy::N; ++i) {
+      const int j = min(key0 + tc.wave_row() + i * Copy::STEP, (end - 1) & ~(Copy::RW - 1));
+      page[i] = pages.number(pg, j);
+      off[i] = j & (pg.size - 1);
+    }
+#pragma unroll
+    for (int i = 0; i < Copy::N; ++i) page[i] = max(uniform(page[i]), 0);
+    tc.wide_bases(kt, a.s.D, (uint32_t)a.k.sr, [&](int i) { return kb + page[i] * pg.page_stride_k + off[i] * a.k.sr; });
+    tc.wide_bases(vt, a.s.C, (uint32_t)a.v.sr, [&](int i) { return vb + page[i] * pg.page_stride_v + off[i] * a.v.sr; });
+    return;
+  }
+  auto key_of = [&](int i) { return min(key0 + tc.row0 + i * Copy::STEP, end - 1); };
+  auto page = [&](int i) { return max(pages.number(pg, key_of(i)), 0); };
+  auto krow = [&](int i) { return page_row(pg, kb, pg.page_stride_k, a.k.sr, page(i), key_of(i)); };
+  auto vrow = [&](int i) { return page_row(pg, vb, pg.page_stride_v, a.v.sr, page(i), key_of(i)); };
+  if (WIDE) {
+    tc.wide_rows(kt, a.s.D, krow);
+    tc.wide_rows(vt, a.s.C, vrow);
+  } else {
+    tc.narrow_rows(kt, a.s.D, krow);
+    tc.narrow_rows(vt, a.s.C, vrow);
+  }
+}
+
 // Sets the bits of the lane's results that infinities among the values of a tile
 // reach: +inf in the first NB words of each column tile, -inf in the next, NaN in
 // both (inf - inf is NaN).  The values are
@@ -439,18 +474,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
   // masked, and stay in the array).
   auto issue = [&](int key0, int stage, int end) {
     char* t = smem + stage * 2 * TILE;
-    auto key_of = [&](int i) { return min(key0 + tc.row0 + i * tc.STEP, (PAGED ? end : kn) - 1); };
+    auto key_of = [&](int i) { return min(key0 + tc.row0 + i * tc.STEP, kn - 1); };
     if constexpr (PAGED) {
-      auto page = [&](int i) { return max(pages.number(a.pg, key_of(i)), 0); };
-      auto krow = [&](int i) { return page_row(a.pg, kb, a.pg.page_stride_k, a.k.sr, page(i), key_of(i)); };
-      auto vrow = [&](int i) { return page_row(a.pg, vb, a.pg.page_stride_v, a.v.sr, page(i), key_of(i)); };
-      if constexpr (WIDE) {
-        tc.wide_rows(t, s.D, krow);
-        tc.wide_rows(t + TILE, s.C, vrow);
-      } else {
-        tc.narrow_rows(t, s.D, krow);
-        tc.narrow_rows(t + TILE, s.C, vrow);
-      }
+      copy_pages<WIDE>(a, pages, tc, t, t + TILE, kb, vb, key0, end);
     } else if constexpr (WIDE) {
       tc.wide(t, kb + (int64_t)key0 * a.k.sr, (uint32_t)a.k.sr, kn - 1 - key0, s.D);
       tc.wide(t + TILE, vb + (int64_t)key0 * a.v.sr, (uint32_t)a.v.sr, kn - 1 - key0, s.C);
@@ -554,18 +580,9 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
   PageSlice pages;
   auto issue = [&](int key0, int stage, int end) {
     char* t = ring + stage * 2 * TILE;
-    auto key_of = [&](int i) { return min(key0 + tc.row0 + i * tc.STEP, (PAGED ? end : kn) - 1); };
+    auto key_of = [&](int i) { return min(key0 + tc.row0 + i * tc.STEP, kn - 1); };
     if constexpr (PAGED) {
-      auto page = [&](int i) { return max(pages.number(a.pg, key_of(i)), 0); };
-      auto krow = [&](int i) { return page_row(a.pg, kb, a.pg.page_stride_k, a.k.sr, page(i), key_of(i)); };
-      auto vrow = [&](int i) { return page_row(a.pg, vb, a.pg.page_stride_v, a.v.sr, page(i), key_of(i)); };
-      if constexpr (WIDE) {
-        tc.wide_rows(t, s.D, krow);
-        tc.wide_rows(t + TILE, s.C, vrow);
-      } else {
-        tc.narrow_rows(t, s.D, krow);
-        tc.narrow_rows(t + TILE, s.C, vrow);
-      }
+      copy_pages<WIDE>(a, pages, tc, t, t + TILE, kb, vb, key0, end);
     } else if constexpr (WIDE) {
       tc.wide(t, kb + (int64_t)key0 * a.k.sr, (uint32_t)a.k.sr, kn - 1 - key0, s.D);
       tc.wide(t + TILE, vb + (int64_t)key0 * a.v.sr, (uint32_t)a.v.sr, kn - 1 - key0, s.C);
@@ -646,6 +663,9 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
 }
 
 // Joins the parts of rows whose keys were split: one wave a row and query head.
+// Lane p holds part p's offset and sum (at most 64 parts); the columns go four a
+// lane, and lanes left over take every second (fourth) part.
+constexpr int kMostParts = 64;
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
   const AttnShape& s = a.s;
@@ -672,26 +692,42 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
     if (lse && lane == 0 && (s.zero_rest & kRestLse)) *lse = -__builtin_inff();
     return;
   }
-  float top = kNoOffset, z = 0.0f;
-  for (int p = 0; p < a.splits; ++p) top = fmaxf(top, a.part_z[2 * (p * units + unit)]);
-  for (int p = 0; p < a.splits; ++p)
-    z += a.part_z[2 * (p * units + unit) + 1] * __builtin_amdgcn_exp2f(a.part_z[2 * (p * units + unit)] - top);
+  float off = kNoOffset, z = 0.0f;
+  if (lane < a.splits) {
+    const floatx2 p = *reinterpret_cast<const floatx2*>(a.part_z + 2 * (lane * units + unit));
+    off = p[0], z = p[1];
+  }
+  float top = off;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float w = __builtin_amdgcn_exp2f(off - top);
+  z *= w;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) z += __shfl_xor(z, d);
   const bool empty = z == 0.0f;
   const float inv = 1.0f / z;
-  for (int c = lane * 4; c < s.C; c += 256) {
-    floatx4 y{0, 0, 0, 0};
-    for (int p = 0; p < a.splits; ++p) {
-      const float w = __builtin_amdgcn_exp2f(a.part_z[2 * (p * units + unit)] - top);
-      const float* o = a.part_o + (p * units + unit) * s.C + c;
-      if ((s.C & 3) == 0) {
-        y += *reinterpret_cast<const floatx4*>(o) * w;
-      } else {
+  const int span = s.C > 128 ? 64 : s.C > 64 ? 32 : 16, groups = 64 / span, group = lane / span;
+  const int c = 4 * (lane & (span - 1));
+  floatx4 y{0, 0, 0, 0};
+#pragma unroll 8
+  for (int p0 = 0; p0 < a.splits; p0 += groups) {
+    const int p = p0 + group;
+    const float wp = __shfl(w, p & 63);
+    if (p >= a.splits || c >= s.C) continue;
+    const float* o = a.part_o + (p * units + unit) * s.C + c;
+    if ((s.C & 3) == 0) {
+      y += *reinterpret_cast<const floatx4*>(o) * wp;
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] += c + e < s.C ? o[e] * w : 0.0f;
-      }
+      for (int e = 0; e < 4; ++e) y[e] += c + e < s.C ? o[e] * wp : 0.0f;
     }
+  }
+  for (int d = span; d < 64; d <<= 1)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : y[e] * inv;
+    for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], d);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : y[e] * inv;
+  if (group == 0) {
     store4<T>(out, c, s.C, a.out.vec, y[0], y[1], y[2], y[3]);
     if (low) store4<T>(low, c, s.C, a.low.vec, left<T>(y[0]), left<T>(y[1]), left<T>(y[2]), left<T>(y[3]));
   }
