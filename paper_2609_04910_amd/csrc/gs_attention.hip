@@ -247,8 +247,8 @@ FwdPlan fwd_plan(const gs_attention_problem& p, bool paged, int64_t keys, void* 
   f.rows = !few ? attn_fwd_rows(DP) : shared <= 16 ? 16 : rows_most(DP);
   f.tiles = tiles_of(p, p.M * f.per, f.rows);
   f.heads = (f.per > 1 || G == 1 ? p.Hkv : p.Hq) * B;
-  // With few workgroups a row's keys are cut into parts
-  const int64_t wgs = f.tiles * f.heads, want = few ? 512 : 512, least = few ? 256 : 512;
+  // With fewer workgroups than two a CU a row's keys are cut into parts
+  const int64_t wgs = f.tiles * f.heads, want = 512, least = few ? kLeastPart : 512;
   f.splits = wgs > 0 && keys >= 2 * least
                  ? std::max<int64_t>(1, std::min({want / wgs, keys / least, (int64_t)kMostParts}))
                  : 1;
@@ -267,6 +267,7 @@ int64_t cache_keys(const gs_attention_cache& c) { return std::min(c.table_width 
 
 void plan_args(const FwdPlan& f, const gs_attention_problem& p, AttnFwdArgs& a) {
   a.per = (int32_t)f.per, a.tiles = (int32_t)f.tiles, a.heads = (int32_t)f.heads;
+  a.wgs = (int32_t)(f.tiles * f.heads);
   a.splits = (int32_t)f.splits, a.part_o = f.part_o, a.part_z = f.part_z;
   a.neg = p.scale < 0;
   a.c = forward_factor(p.scale);

@@ -37,6 +37,7 @@ struct AttnFwdArgs {
   int32_t heads;           // heads of the grid, all sequences of a dense call together
   int32_t neg;             // scale < 0: queries enter negated
   float c;                 // |scale| log2 e
+  int32_t wgs;             // workgroups of one part
   int32_t splits;          // parts that a row's keys are cut into (1: results are written at once)
   float* part_o;           // splits x rows x query heads x C: sums of weights times values
   float* part_z;           // splits x rows x query heads x 2: offset and sum of weights
@@ -224,18 +225,37 @@ struct AttnJob {
   int part;            // which split
 };
 
+// The sequence with the rank-th longest of B lengths (equal ones by number), so
+// that a batch's long sequences start first and its short ones fill in: 64
+// sequences of 2048 to 8192 keys, 8 key heads 333 -> 278 us (5.1 TB/s; equal lengths of 4096
+// 205 -> 211 us).  One lane a sequence;
+// more sequences than lanes even out by their number.
+__device__ __forceinline__ int by_length(const int32_t* lens, int B, int rank) {
+  if (B > 64) return rank;
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < B ? clampi(lens[lane], 0, (1 << 25) - 1) << 6 | (63 - lane) : -1;
+  int place = 0;
+#pragma unroll 8
+  for (int b = 0; b < B; ++b) place += __builtin_amdgcn_readlane(mine, b) > mine;
+  return __builtin_ctzll(__ballot(lane < B && place == rank));
+}
+
 // Returns whether there is anything to do (rows of no sequence are handled here).
-template <int ROWS, bool PAGED>
+// SORT: where no two workgroups share keys, the sequences of most keys first.
+template <int ROWS, bool PAGED, bool SORT>
 __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
   const AttnShape& s = a.s;
   int id = blockIdx.x;
   w.part = 0;
   if (a.splits > 1) {
-    w.part = id % a.splits;
-    id /= a.splits;
+    // all first parts, then all second ones, ...: parts without keys then fall on
+    // every XCD alike
+    w.part = id / a.wgs;
+    id -= w.part * a.wgs;
   }
   int tile, head;
   block_place(id, a.heads, tile, head);
+  const int tile_id = tile;
   if (s.packed) {
     const int slot = a.tiles - 1 - tile;
     w.b = packed_tile(s.q_index, s.B, s.M, a.per, ROWS, slot, tile);
@@ -257,8 +277,14 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
     }
   } else {
     const int per_seq = a.heads / s.B;
-    w.b = head / per_seq;
-    head -= w.b * per_seq;
+    if (SORT) {
+      const int p = id - tile_id * a.heads;
+      w.b = by_length(a.pg.lens, s.B, p / per_seq);
+      head = p % per_seq;
+    } else {
+      w.b = head / per_seq;
+      head -= w.b * per_seq;
+    }
     tile = a.tiles - 1 - tile;  // the tiles that see most keys first
   }
   w.head = head;
@@ -295,13 +321,14 @@ __device__ __forceinline__ KeyRange keys_of_rows(const AttnFwdArgs& a, const Att
   return r;
 }
 
-// This workgroup's part of the keys [lo, hi): cut into `splits` parts of whole
-// tiles, no part shorter than 256 keys.
+// This workgroup's part of the keys [lo, hi): whole tiles, no part shorter than
+// kLeastPart keys.
+constexpr int kLeastPart = 256;
 __device__ __forceinline__ void split_keys(const AttnFwdArgs& a, const AttnJob& w, int tile, int& lo, int& hi) {
   lo = lo / tile * tile;
   if (a.splits == 1) return;
-  int each = (hi - lo + a.splits - 1) / a.splits;
-  each = (max(each, 256) + tile - 1) / tile * tile;
+  int each = max(kLeastPart, (hi - lo + a.splits - 1) / a.splits);
+  each = (each + tile - 1) / tile * tile;
   const int64_t first = lo + (int64_t)w.part * each;
   hi = first < hi ? (int)min(first + each, (int64_t)hi) : lo;
   lo = first < hi ? (int)first : lo;
@@ -417,6 +444,8 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
   const int64_t row = w.sq.q0 + token;
   if (a.splits > 1) {
     const int64_t at = ((w.part * (int64_t)(s.packed ? 1 : s.B) + (s.packed ? 0 : w.b)) * s.M + row) * s.Hq + h;
+    if (first) a.part_z[2 * at] = off, a.part_z[2 * at + 1] = z;
+    if (off == kNoOffset) return;  // no keys: the sums are not looked at
     float* p = a.part_o + at * s.C + c;
     if ((s.C & 3) == 0) {
       if (c < s.C) *reinterpret_cast<floatx4*>(p) = o;
@@ -425,7 +454,6 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
       for (int e = 0; e < 4; ++e)
         if (c + e < s.C) p[e] = o[e];
     }
-    if (first) a.part_z[2 * at] = off, a.part_z[2 * at + 1] = z;
     return;
   }
   const bool empty = rest || z == 0.0f;
@@ -456,7 +484,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 
   AttnJob job;
-  if (!attn_job<ROWS, PAGED>(a, job)) return;
+  if (!attn_job<ROWS, PAGED, false>(a, job)) return;
   const int kn = job.sq.kn, wr0 = job.r0 + wave * 16 * NQ;
   AttnRows<T, DP, NQ> rows;
   rows.start(a, job, wr0);
@@ -564,7 +592,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 
   AttnJob job;
-  if (!attn_job<ROWS, PAGED>(a, job)) return;
+  if (!attn_job<ROWS, PAGED, PAGED>(a, job)) return;
   const int kn = job.sq.kn;
   AttnRows<T, DP, NQ> rows;
   rows.start(a, job, job.r0);
@@ -713,7 +741,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
   for (int p0 = 0; p0 < a.splits; p0 += groups) {
     const int p = p0 + group;
     const float wp = __shfl(w, p & 63);
-    if (p >= a.splits || c >= s.C) continue;
+    if (p >= a.splits || c >= s.C || wp == 0.0f) continue;  // (parts without keys hold no sums)
     const float* o = a.part_o + (p * units + unit) * s.C + c;
     if ((s.C & 3) == 0) {
       y += *reinterpret_cast<const floatx4*>(o) * wp;
