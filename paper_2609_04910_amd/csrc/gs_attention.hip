@@ -28,12 +28,13 @@ namespace gs {
 // waves a SIMD, 256 registers).  Forward of 8192 tokens, 32 heads, D = 128,
 // causal: two tiles 617 us, three 572 us, four 2750 us (spilled); D = 256
 // (2 x 2048 tokens, 8 heads): one 91 us, two 332 us (spilled).  dQ at D = 128: two
-// 807 us, three 1947 us.  dK and dV at D = 128: one 1360 us, two 3574 us, or
-// 1567 us with 512 registers and one wave a SIMD.  Eight waves a workgroup instead
-// of four: 4 to 10 % slower at every width.
+// 807 us, three 1947 us.  dK and dV at D = 128: two, with the operands of V in LDS
+// (2 x 4096 tokens, 32 heads, no mask: 982 us; one tile 1248 us; two with all
+// operands in registers spill).  Eight waves a workgroup instead of four: 4 to
+// 10 % slower at every width.
 constexpr int kAttnWaves = 4;
 constexpr int attn_nq(int DP) { return DP == 256 ? 1 : DP == 128 ? 3 : 2; }
-constexpr int attn_nt(int DP, bool KV) { return DP == 256 || (KV && DP == 128) ? 1 : 2; }
+constexpr int attn_nt(int DP, bool KV) { return DP == 256 ? 1 : 2; }
 
 // Few rows (k_attn_rows): one tile of 16 rows or four (DP = 256: one; four do not
 // fit the registers), and as many waves as their rings fit in LDS.
@@ -52,8 +53,9 @@ hipError_t launch(K kernel, int64_t grid, int threads, const A& args, hipStream_
 // rows: rows of a tile; at most rows_most(DP): k_attn_rows
 template <typename T, int DP>
 hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int rows, int64_t grid, hipStream_t st);
+// cols: columns of a workgroup, attn_bwd_cols(DP, kv) or (dK and dV at DP = 128) half of them
 template <typename T, int DP>
-hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st);
+hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int cols, int64_t grid, hipStream_t st);
 
 #if GS_PART != 0
 template <typename T, int DP, int NQ, bool PAGED>
@@ -82,18 +84,27 @@ hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int rows, int64_t grid, hi
   const int64_t units = (int64_t)(a.s.packed ? 1 : a.s.B) * a.s.M * a.s.Hq;
   return launch(&k_attn_join<T>, (units + 3) / 4, 256, a, st);
 }
+template <typename T, int DP, int NT, bool KV>
+hipError_t attn_pass(const AttnBwdArgs& a, int64_t grid, hipStream_t st) {
+  const bool wide = KV ? a.q.vec && a.dout.vec : a.k.vec && a.v.vec;
+  return launch(wide ? &k_attn_bwd<T, DP, NT, kAttnWaves, KV, true> : &k_attn_bwd<T, DP, NT, kAttnWaves, KV, false>,
+                grid, 64 * kAttnWaves, a, st);
+}
 template <typename T, int DP>
-hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int64_t grid, hipStream_t st) {
-  constexpr int NQ = attn_nt(DP, false), NK = attn_nt(DP, true), NW = kAttnWaves;
-  const bool wide = kv ? a.q.vec && a.dout.vec : a.k.vec && a.v.vec;
-  return launch(kv ? wide ? &k_attn_bwd<T, DP, NK, NW, true, true> : &k_attn_bwd<T, DP, NK, NW, true, false>
-                : wide ? &k_attn_bwd<T, DP, NQ, NW, false, true>
-                       : &k_attn_bwd<T, DP, NQ, NW, false, false>,
-                grid, 64 * NW, a, st);
+hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int cols, int64_t grid, hipStream_t st) {
+  if (!kv) return attn_pass<T, DP, attn_nt(DP, false), false>(a, grid, st);
+  hipError_t e;
+  if (DP == 128 && cols < attn_bwd_cols(DP, true))
+    e = attn_pass<T, DP, DP == 128 ? 1 : attn_nt(DP, true), true>(a, grid, st);
+  else
+    e = attn_pass<T, DP, attn_nt(DP, true), true>(a, grid, st);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t units = (int64_t)(a.s.packed ? 1 : a.s.B) * a.s.N * a.s.Hkv;
+  return launch(&k_attn_sum<T>, (units + 3) / 4, 256, a, st);
 }
 #define GS_ATTN_INSTANCE(T, DP)                                                               \
   template hipError_t attn_fwd<T, DP>(const AttnFwdArgs&, bool, int, int64_t, hipStream_t);   \
-  template hipError_t attn_bwd<T, DP>(const AttnBwdArgs&, bool, int64_t, hipStream_t);
+  template hipError_t attn_bwd<T, DP>(const AttnBwdArgs&, bool, int, int64_t, hipStream_t);
 #if GS_PART == 1 || GS_PART == -1
 GS_ATTN_INSTANCE(F16, 64)
 #endif
@@ -273,19 +284,52 @@ void plan_args(const FwdPlan& f, const gs_attention_problem& p, AttnFwdArgs& a) 
   a.c = forward_factor(p.scale);
 }
 
-struct BwdWork {
-  float *norms, *delta, *lse2;
+// How a backward call is laid out: columns of a workgroup of the dK, dV pass, the
+// grids of both passes, workgroups that share a key head's query heads, workspace.
+struct BwdPlan {
+  int k_cols;
+  int64_t q_tiles, q_heads, k_tiles, k_heads, splits;
+  float *norms, *delta, *lse2, *part;
+  int64_t part_width;
   size_t total;
 };
 
-BwdWork bwd_work(const gs_attention_problem& p, void* ws) {
+BwdPlan bwd_plan(const gs_attention_problem& p, bool want_kv, void* ws) {
+  BwdPlan f{};
+  const int DP = padded_width(p.D, p.C);
+  const int64_t B = p.packed ? 1 : p.B, G = p.Hq / p.Hkv;
+  f.q_tiles = tiles_of(p, p.M, attn_bwd_cols(DP, false)), f.q_heads = p.Hq * B;
+  f.k_heads = p.Hkv * B;
+  f.k_cols = attn_bwd_cols(DP, true);
+  f.k_tiles = tiles_of(p, p.N, f.k_cols);
+  // dK, dV: 512 workgroups fill the GPU (two a CU); with a causal mask, whose tiles
+  // have unequal numbers of pairs, it takes 1024 to even out.  Where there are fewer
+  // the query heads of a key head are shared by several workgroups, as far as they
+  // go (causal: to 2048, since the sums cost a pass anyway), and then at D = 128
+  // tiles of half the columns are taken.  8192 tokens, 32 heads over 8, causal: 512
+  // workgroups 1531 us, 1024 half tiles 1380 us, heads shared by two 1237 us, by
+  // four 1181 us; 4 x 4096 tokens (1024 workgroups): not shared 1156 us, by two
+  // 1228 us.
+  const bool even = !p.causal || (p.window > 0 && 2 * p.window <= p.N) || (p.packed && p.B >= 4);
+  const int64_t want = even ? 512 : 1024, wgs = f.k_tiles * f.k_heads;
+  f.splits = 1;
+  if (wgs < want)
+    while (f.splits < G && wgs * f.splits < (even ? want : 2 * want)) {
+      do ++f.splits;
+      while (G % f.splits);
+    }
+  if (DP == 128 && f.k_tiles * f.k_heads * f.splits < want) {
+    f.k_cols /= 2;
+    f.k_tiles = tiles_of(p, p.N, f.k_cols);
+  }
   Carve c{static_cast<char*>(ws)};
-  BwdWork w;
-  w.norms = c.take<float>(2 * kNormBlocks);
-  w.delta = c.take<float>(row_heads(p));
-  w.lse2 = c.take<float>(row_heads(p));
-  w.total = c.off;
-  return w;
+  f.norms = c.take<float>(2 * kNormBlocks);
+  f.delta = c.take<float>(row_heads(p));
+  f.lse2 = c.take<float>(row_heads(p));
+  f.part_width = 2 * ((std::max(p.D, p.C) + 3) / 4 * 4);
+  if (want_kv && f.splits > 1) f.part = c.take<float>(f.splits * B * p.N * p.Hkv * f.part_width);
+  f.total = c.off;
+  return f;
 }
 
 gs_status check_workspace(const void* ws, size_t have, size_t need) {
@@ -376,6 +420,8 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
   if (p->B == 0 || (p->M == 0 && p->N == 0)) return GS_SUCCESS;
   if ((st = index_args(*p, q_index, k_index)) != GS_SUCCESS) return st;
   const int64_t B = p->packed ? 1 : p->B;
+  const BwdPlan w = bwd_plan(*p, dk || dv, ws);
+  if (w.q_tiles * w.q_heads > kMaxGrid || w.k_tiles * w.k_heads * w.splits > kMaxGrid) return GS_ERR_BAD_SHAPE;
   AttnBwdArgs a{};
   AttnArray ao, alow{};
   Span in[9], o[4];
@@ -393,12 +439,10 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
   if (reinterpret_cast<uintptr_t>(lse) & 3) return GS_ERR_MISALIGNED;
   if (lse) in[5] = span_of(lse, 4 * row_heads(*p));
   in[6] = index_span(*p, q_index), in[7] = index_span(*p, k_index);
-  const BwdWork w = bwd_work(*p, ws);
   if ((st = check_workspace(ws, ws_bytes, w.total)) != GS_SUCCESS) return st;
   o[3] = span_of(ws, (int64_t)w.total);
   if (overlaps(o, 4, in, 9)) return GS_ERR_ALIAS;
 
-  const int DP = padded_width(p->D, p->C);
   a.s = shape_of(*p, q_index, k_index);
   a.lse2 = w.lse2;
   a.delta = w.delta;
@@ -425,11 +469,6 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
   pr.k_blocks = (int32_t)std::min(most, (pr.k_units + 15) / 16);
   a.q_blocks = pr.q_blocks, a.k_blocks = pr.k_blocks;
 
-  const int64_t q_tiles = tiles_of(*p, p->M, attn_bwd_cols(DP, false)), q_heads = p->Hq * B;
-  const int64_t k_tiles = tiles_of(*p, p->N, attn_bwd_cols(DP, true)), k_heads = p->Hkv * B;
-  if (q_tiles * q_heads > kMaxGrid || k_tiles * k_heads > kMaxGrid)
-    return GS_ERR_BAD_SHAPE;
-
   hipError_t e = hipSuccess;
   const int blocks = pr.q_blocks + pr.k_blocks;
   if (blocks > 0)
@@ -438,10 +477,13 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
   if (e != hipSuccess) return GS_ERR_HIP;
   for (int kv = 0; kv < 2; ++kv) {
     if (kv ? (!dk && !dv) || p->N == 0 : !dq || p->M == 0) continue;
-    a.tiles = (int32_t)(kv ? k_tiles : q_tiles);
-    a.heads = (int32_t)(kv ? k_heads : q_heads);
+    a.tiles = (int32_t)(kv ? w.k_tiles : w.q_tiles);
+    a.heads = (int32_t)(kv ? w.k_heads : w.q_heads);
+    a.splits = kv ? (int32_t)w.splits : 1;
+    a.wgs = a.tiles * a.heads;
+    a.part = w.part, a.part_width = (int32_t)w.part_width;
     e = by_type(*p, [&](auto t, auto dp) {
-      return attn_bwd<decltype(t), decltype(dp)::value>(a, kv != 0, (int64_t)a.tiles * a.heads, stream);
+      return attn_bwd<decltype(t), decltype(dp)::value>(a, kv != 0, w.k_cols, (int64_t)a.wgs * a.splits, stream);
     });
     if (e != hipSuccess) return GS_ERR_HIP;
   }
@@ -565,7 +607,7 @@ gs_status gs_attention_fwd(const gs_attention_problem* p, const gs_attention_arr
 
 size_t gs_attention_bwd_workspace_size(const gs_attention_problem* p, int want_dq, int want_dk, int want_dv) {
   if (gs::check(p) != GS_SUCCESS || (!want_dq && !want_dk && !want_dv)) return 0;
-  return gs::bwd_work(*p, nullptr).total;
+  return gs::bwd_plan(*p, want_dk || want_dv, nullptr).total;
 }
 
 gs_status gs_attention_bwd(const gs_attention_problem* p, const gs_attention_array* q, const gs_attention_array* k,

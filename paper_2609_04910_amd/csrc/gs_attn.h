@@ -116,10 +116,16 @@ __device__ __forceinline__ int packed_tile(const int32_t* off, int B, int rows, 
 // eight XCDs in turn, and each XCD has an L2 of its own: with a multiple of eight
 // (sequence, head) streams every XCD gets a contiguous run of them, so the query
 // heads that share a key head read its keys through one L2.
-__device__ __forceinline__ void block_place(int id, int heads, int& tile, int& head) {
+//
+// The caller counts tiles from the one with most pairs (causal masks).  The first
+// 256 blocks go to a CU each and the next 256 join them: those are turned round, so
+// that the CU of the longest block gets the shortest of them.
+__device__ __forceinline__ void block_place(int id, int heads, int tiles, int& tile, int& head) {
   tile = id / heads;
   const int p = id - tile * heads;
   head = (heads & 7) == 0 ? (p & 7) * (heads >> 3) + (p >> 3) : p;
+  const int row = 256 / heads;
+  if (tile >= row && tile < 2 * row) tile = row + min(2 * row, tiles) - 1 - tile;
 }
 
 // Rows that column point `at` (its index in its sequence) sees on the other
@@ -328,25 +334,56 @@ __device__ __forceinline__ uint4 tr_operand(const char* tile, const TileLane<DP>
   return uint4{a.x, a.y, b.x, b.y};
 }
 
-// Nothing moves across: keeps a stage's LDS reads one stage ahead of the
+// No LDS access and no matrix instruction moves across (vector arithmetic may):
+// keeps a stage's LDS reads one stage ahead of the
 // matrix instructions that use them.  Left to itself the compiler issues a whole
 // phase's reads at once, and holds them in registers that the sums need (the
 // D = 128 kernels then spilled 50 to 450 values inside the tile loop).
-__device__ __forceinline__ void stage_fence() { __builtin_amdgcn_sched_barrier(0); }
+__device__ __forceinline__ void stage_fence() { __builtin_amdgcn_sched_barrier(0x6); }
+
+// Operands are read kAhead stages before the matrix instructions that use them.
+constexpr int kAhead = 2;
 
 // s[n] += X U[n] over NC chunks of 32 columns: rows 16 t .. of a tile.
 template <typename T, int DP, int NT>
 __device__ __forceinline__ void scores(const char* tile, const TileLane<DP>& ln, int t, const uint4 (&u)[NT][DP / 32],
                                        floatx4 (&s)[NT]) {
-  constexpr int NC = DP / 32;
-  uint4 x[2];
-  x[0] = row_operand<DP>(tile, ln, t, 0);
+  constexpr int NC = DP / 32, P = kAhead < NC ? kAhead : NC - 1;
+  uint4 x[P + 1];
+#pragma unroll
+  for (int c = 0; c < P; ++c) x[c] = row_operand<DP>(tile, ln, t, c);
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    if (c + 1 < NC) x[(c + 1) & 1] = row_operand<DP>(tile, ln, t, c + 1);
+    if (c + P < NC) x[(c + P) % (P + 1)] = row_operand<DP>(tile, ln, t, c + P);
     stage_fence();
 #pragma unroll
-    for (int n = 0; n < NT; ++n) s[n] = mfma_qk<T>(x[c & 1], u[n][c], s[n]);
+    for (int n = 0; n < NT; ++n) s[n] = mfma_qk<T>(x[c % (P + 1)], u[n][c], s[n]);
+    stage_fence();
+  }
+}
+
+// d[t][n] += Y W[n] for the two row tiles of step s, with the column operands W
+// read from LDS as well (rows 16 n .. of `cols`).
+template <typename T, int DP, int NT>
+__device__ __forceinline__ void scores_lds(const char* tile, const char* cols, const TileLane<DP>& ln, int s,
+                                           floatx4 (&d)[2][NT]) {
+  constexpr int NC = DP / 32;
+  uint4 y[2][2], w[2][NT];
+  auto read = [&](int c) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) w[c & 1][n] = row_operand<DP>(cols, ln, n, c);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) y[c & 1][t] = row_operand<DP>(tile, ln, 2 * s + t, c);
+  };
+  read(0);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    if (c + 1 < NC) read(c + 1);
+    stage_fence();
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) d[t][n] = mfma_qk<T>(y[c & 1][t], w[c & 1][n], d[t][n]);
     stage_fence();
   }
 }
@@ -356,14 +393,16 @@ __device__ __forceinline__ void scores(const char* tile, const TileLane<DP>& ln,
 template <typename T, int DP, int NC, int NT>
 __device__ __forceinline__ void contract(const char* tile, const TileLane<DP>& ln, int s, const uint4 (&b)[NT],
                                          floatx4 (&acc)[NC][NT]) {
-  uint4 a[2];
-  a[0] = tr_operand<DP>(tile, ln, s, 0);
+  constexpr int P = kAhead < NC ? kAhead : NC - 1;
+  uint4 a[P + 1];
+#pragma unroll
+  for (int ct = 0; ct < P; ++ct) a[ct] = tr_operand<DP>(tile, ln, s, ct);
 #pragma unroll
   for (int ct = 0; ct < NC; ++ct) {
-    if (ct + 1 < NC) a[(ct + 1) & 1] = tr_operand<DP>(tile, ln, s, ct + 1);
+    if (ct + P < NC) a[(ct + P) % (P + 1)] = tr_operand<DP>(tile, ln, s, ct + P);
     stage_fence();
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[ct][n] = mfma_qk<T>(a[ct & 1], b[n], acc[ct][n]);
+    for (int n = 0; n < NT; ++n) acc[ct][n] = mfma_qk<T>(a[ct % (P + 1)], b[n], acc[ct][n]);
     stage_fence();
   }
 }
@@ -395,6 +434,28 @@ __device__ __forceinline__ bool clean_tile(char* tile, int tid) {
 }
 
 // ------------------------------------------------------------- 16-bit output
+
+// Four neighbouring 32-bit sums of a row of `width`.
+__device__ __forceinline__ void store_sums(float* row, int c, int width, const floatx4& x) {
+  if ((width & 3) == 0) {
+    if (c < width) *reinterpret_cast<floatx4*>(row + c) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < width) row[c + e] = x[e];
+  }
+}
+__device__ __forceinline__ floatx4 load_sums(const float* row, int c, int width) {
+  floatx4 x{0, 0, 0, 0};
+  if ((width & 3) == 0) {
+    if (c < width) x = *reinterpret_cast<const floatx4*>(row + c);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < width) x[e] = row[c + e];
+  }
+  return x;
+}
 
 // Four neighbouring columns of one row, rounded to T once.
 template <typename T>

@@ -29,6 +29,10 @@ struct AttnBwdArgs {
   int32_t q_blocks, k_blocks;  // and how many there are
   int32_t tiles, heads;    // as in AttnFwdArgs
   float c;                 // scale log2 e
+  int32_t splits;          // dK, dV: workgroups that share the query heads of a key head
+  int32_t wgs;             // workgroups of one split
+  int32_t part_width;      // twice the wider of D and C, rounded up to fours
+  float* part;             // with several: splits x rows x key heads x part_width sums, of dK and then dV
 };
 
 // fp16: kernel weights enter dV times 2^15 (a weight of 2^-16, one key of 65536,
@@ -173,24 +177,30 @@ __device__ __forceinline__ bool row_not_finite(const char* row, int width) {
   return bad;
 }
 
+// Whether the column operands of dP lie in LDS instead of registers.
+constexpr bool attn_bwd_lds(int DP, int NT, bool KV) { return KV && DP == 128 && NT == 2; }
+
 template <typename T, int DP, int NT, int NW, bool KV, bool WIDE>
 __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
-  constexpr int BR = attn_keys<DP>(), NC = DP / 32, NO = DP / 16, TILE = BR * DP * 2, COLS = 16 * NT * NW;
+  constexpr bool WLDS = attn_bwd_lds(DP, NT, KV);
+  constexpr int BR = WLDS ? 32 : attn_keys<DP>(), NC = DP / 32, NO = DP / 16, TILE = BR * DP * 2, COLS = 16 * NT * NW;
   __shared__ __align__(1024) char smem[4 * TILE];
   __shared__ __align__(16) float stat[2][2][BR];  // [stage][lse, delta][row]
   __shared__ int mark[4];
+  __shared__ __align__(1024) char wcols[WLDS ? COLS * DP * 2 : 16];
   const AttnShape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
 
   int tile, head, b;
-  block_place(blockIdx.x, a.heads, tile, head);
+  const int split = KV ? blockIdx.x / a.wgs : 0;
+  block_place(blockIdx.x - split * a.wgs, a.heads, a.tiles, tile, head);
   const int rows_all = KV ? s.N : s.M;
   if (s.packed) {
     const int slot = KV ? tile : a.tiles - 1 - tile;
     b = packed_tile(KV ? s.k_index : s.q_index, s.B, rows_all, 1, COLS, slot, tile);
     if (b == kNoRow) {
-      if (s.zero_rest & kRestOut) {
+      if ((s.zero_rest & kRestOut) && split == 0) {
         const int part = slot - tile, parts = a.tiles - tile;
         const int32_t* index = KV ? s.k_index : s.q_index;
         const int end = s.B > 0 ? clampi(index[s.B], 0, rows_all) : 0;
@@ -221,7 +231,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
 
   const int wc0 = t0 + wave * 16 * NT;
   int lo[NT], hi[NT];
-  uint4 uo[NT][NC], wo[NT][NC];
+  uint4 uo[NT][NC], wo[WLDS ? 1 : NT][NC];
+  char* wmine = wcols + (WLDS ? wave * 16 * NT * DP * 2 : 0);
   float clse[NT], cdelta[NT];
   auto range = [&](int at, int& l, int& h) {
     if (KV)
@@ -241,7 +252,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         uo[n][c] = column_operand<T>(u, U.vec, s.D, c, 0);
-        wo[n][c] = column_operand<T>(w, W.vec, s.C, c, 0);
+        const uint4 x = column_operand<T>(w, W.vec, s.C, c, 0);
+        if (WLDS)
+          *reinterpret_cast<uint4*>(wmine + (16 * n + col) * DP * 2 + ((4 * c + g) ^ swz(col)) * 16) = x;
+        else
+          wo[WLDS ? 0 : n][c] = x;
       }
       if (!KV) {
         const int64_t i = b * a.st_sb + head * a.st_sh + c0 + at;
@@ -274,7 +289,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
 
   const TileLane<DP> ln;
   // the stream: tiles of rows [r_lo, r_hi), once for every query head (KV)
-  const int heads = KV ? s.G : 1, h0 = KV ? head * s.G : head / s.G;
+  const int heads = KV ? s.G / a.splits : 1, h0 = KV ? head * s.G + split * heads : head / s.G;
   const int steps = r_hi > r_lo ? (r_hi - r_lo + BR - 1) / BR : 0;
   const TileCopy<DP, BR, 64 * NW> tc(tid);
   auto issue = [&](int h, int row0, int stage) {
@@ -337,20 +352,30 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
 #pragma unroll
       for (int hf = 0; hf < BR / 32; ++hf) {
         uint32_t pw[NT][4], dsw[NT][4];
+        floatx4 sc2[2][NT], dp2[2][NT];
+        // dP - delta: the sums start at -delta
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          floatx4 sc[NT], dp[NT];
-          floatx4 rl{0, 0, 0, 0};
-          // dP - delta: the sums start at -delta
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            sc[n] = floatx4{0, 0, 0, 0};
-            dp[n] = KV ? -*reinterpret_cast<const floatx4*>(&stat[stage][1][32 * hf + 16 * t + 4 * g])
-                       : floatx4{-cdelta[n], -cdelta[n], -cdelta[n], -cdelta[n]};
+            sc2[t][n] = floatx4{0, 0, 0, 0};
+            dp2[t][n] = KV ? -*reinterpret_cast<const floatx4*>(&stat[stage][1][32 * hf + 16 * t + 4 * g])
+                           : floatx4{-cdelta[n], -cdelta[n], -cdelta[n], -cdelta[n]};
           }
+        if constexpr (WLDS) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) scores<T, DP, NT>(xt, ln, 2 * hf + t, uo, sc2[t]);
+          scores_lds<T, DP, NT>(yt, wmine, ln, hf, dp2);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          floatx4(&sc)[NT] = sc2[t], (&dp)[NT] = dp2[t];
+          floatx4 rl{0, 0, 0, 0};
           if (KV) rl = *reinterpret_cast<const floatx4*>(&stat[stage][0][32 * hf + 16 * t + 4 * g]);
-          scores<T, DP, NT>(xt, ln, 2 * hf + t, uo, sc);
-          scores<T, DP, NT>(yt, ln, 2 * hf + t, wo, dp);
+          if constexpr (!WLDS) {
+            scores<T, DP, NT>(xt, ln, 2 * hf + t, uo, sc);
+            scores<T, DP, NT>(yt, ln, 2 * hf + t, wo, dp);
+          }
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -390,8 +415,19 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int at = wc0 + 16 * n + col;
-    if (at >= limit || (at >= cn && !(s.zero_rest & kRestOut))) continue;
+    if (at >= limit || (at >= cn && (!(s.zero_rest & kRestOut) || split > 0))) continue;
     const bool none = at >= cn;
+    if (KV && a.splits > 1 && !none) {
+      const int64_t row = (s.packed ? 0 : (int64_t)b * s.N) + c0 + at, rows = (int64_t)(s.packed ? 1 : s.B) * s.N;
+      float* p = a.part + ((split * rows + row) * s.Hkv + head) * a.part_width;
+#pragma unroll
+      for (int ct = 0; ct < NO; ++ct) {
+        const float nan = spoilt[n] ? __builtin_nanf("") : 0.0f;
+        store_sums(p, 16 * ct + 4 * g, s.D, du[ct][n] * u_scale + nan);
+        store_sums(p + a.part_width / 2, 16 * ct + 4 * g, s.C, dw[KV ? ct : 0][n] * w_scale + nan);
+      }
+      continue;
+    }
     if (DU.p) {
       char* p = DU.p + b * DU.sb + (int64_t)(c0 + at) * DU.sr + head * DU.sh;
 #pragma unroll
@@ -413,6 +449,34 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       }
     }
   }
+}
+
+// dk and dv from the sums of the workgroups that shared a key head: one wave a row
+// and key head.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_sum(const AttnBwdArgs a) {
+  const AttnShape& s = a.s;
+  const int64_t rows = (int64_t)(s.packed ? 1 : s.B) * s.N, units = rows * s.Hkv;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (unit >= units) return;
+  const int h = (int)(unit % s.Hkv), c = 4 * (threadIdx.x & 63);
+  const int64_t at = unit / s.Hkv;
+  const int b = s.packed ? 0 : (int)(at / s.N);
+  const int64_t row = at - (int64_t)b * s.N;
+  // rows of no sequence are written, or left, by the main kernel
+  if (s.packed) {
+    if (row < clampi(s.k_index[0], 0, s.N) || row >= clampi(s.k_index[s.B], 0, s.N)) return;
+  } else if (s.k_index && row >= clampi(s.k_index[b], 0, s.N)) {
+    return;
+  }
+  floatx4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
+  for (int p = 0; p < a.splits; ++p) {
+    const float* from = a.part + (p * units + unit) * a.part_width;
+    x += load_sums(from, c, s.D);
+    y += load_sums(from + a.part_width / 2, c, s.C);
+  }
+  if (a.dk.p) store4<T>(a.dk.p + b * a.dk.sb + row * a.dk.sr + h * a.dk.sh, c, s.D, a.dk.vec, x[0], x[1], x[2], x[3]);
+  if (a.dv.p) store4<T>(a.dv.p + b * a.dv.sb + row * a.dv.sr + h * a.dv.sh, c, s.C, a.dv.vec, y[0], y[1], y[2], y[3]);
 }
 
 }  // namespace gs

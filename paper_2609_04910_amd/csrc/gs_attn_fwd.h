@@ -254,8 +254,7 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
     id -= w.part * a.wgs;
   }
   int tile, head;
-  block_place(id, a.heads, tile, head);
-  const int tile_id = tile;
+  block_place(id, a.heads, a.tiles, tile, head);
   if (s.packed) {
     const int slot = a.tiles - 1 - tile;
     w.b = packed_tile(s.q_index, s.B, s.M, a.per, ROWS, slot, tile);
@@ -278,7 +277,7 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
   } else {
     const int per_seq = a.heads / s.B;
     if (SORT) {
-      const int p = id - tile_id * a.heads;
+      const int p = id % a.heads;
       w.b = by_length(a.pg.lens, s.B, p / per_seq);
       head = p % per_seq;
     } else {
@@ -446,14 +445,7 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
     const int64_t at = ((w.part * (int64_t)(s.packed ? 1 : s.B) + (s.packed ? 0 : w.b)) * s.M + row) * s.Hq + h;
     if (first) a.part_z[2 * at] = off, a.part_z[2 * at + 1] = z;
     if (off == kNoOffset) return;  // no keys: the sums are not looked at
-    float* p = a.part_o + at * s.C + c;
-    if ((s.C & 3) == 0) {
-      if (c < s.C) *reinterpret_cast<floatx4*>(p) = o;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c + e < s.C) p[e] = o[e];
-    }
+    store_sums(a.part_o + at * s.C, c, s.C, o);
     return;
   }
   const bool empty = rest || z == 0.0f;
@@ -742,13 +734,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
     const int p = p0 + group;
     const float wp = __shfl(w, p & 63);
     if (p >= a.splits || c >= s.C || wp == 0.0f) continue;  // (parts without keys hold no sums)
-    const float* o = a.part_o + (p * units + unit) * s.C + c;
-    if ((s.C & 3) == 0) {
-      y += *reinterpret_cast<const floatx4*>(o) * wp;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += c + e < s.C ? o[e] * wp : 0.0f;
-    }
+    y += load_sums(a.part_o + (p * units + unit) * s.C, c, s.C) * wp;
   }
   for (int d = span; d < 64; d <<= 1)
 #pragma unroll

@@ -64,6 +64,8 @@ SHAPES = [  # B, M, N, Hq, Hkv, D, C, causal, window
     (1, 140, 140, 2, 1, 256, 256, True, 0),
     (1, 70, 40, 2, 1, 200, 129, False, 0),
     (1, 90, 600, 8, 1, 128, 64, True, 0),
+    (4, 1100, 1100, 1, 1, 128, 128, False, 0),
+    (130, 130, 130, 4, 4, 128, 128, False, 0),  # enough workgroups for whole tiles
     # few rows, or few workgroups: the keys are cut into parts
     (1, 1, 5000, 8, 2, 128, 128, False, 0),
     (2, 3, 3000, 4, 4, 64, 64, True, 0),
@@ -182,6 +184,28 @@ def test_lengths_where_keys_are_cut_into_parts(at, M, N):
         exact = ref.one(q[b, :rows[b]], k[b, :keys[b]], v[b, :keys[b]], 0.125, True)["out"][0]
         assert (out[b, :rows[b]].cpu().double() - exact).norm() + 1e-9 >= \
             (out[b, :rows[b]].cpu().double() + low[b, :rows[b]].cpu().double() - exact).norm()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("Hq,Hkv,D,C", [(6, 1, 128, 128), (8, 2, 64, 48), (4, 1, 256, 199), (12, 1, 100, 33)])
+def test_shared_key_heads(at, Hq, Hkv, D, C, dtype):
+    """The query heads of a key head shared by workgroups, their sums joined: padded, packed, causal."""
+    rows, keys = [130, 0, 77], [60, 140, 0]
+    q, k, v, g = make(24, 3, 130, 140, Hq, Hkv, D, C, dtype)
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (rows, keys)]
+    for causal in (False, True):
+        check_dense(at, q, k, v, g, rows=rows, keys=keys, q_lens=lens[0], k_lens=lens[1], causal=causal)
+    offs = [torch.tensor([0, 130, 130, 207], dtype=torch.int32, device="cuda"), torch.tensor([0, 60, 200, 200], dtype=torch.int32, device="cuda")]
+    pk = [torch.cat([t[b, :n[b]] for b in range(3)] + [t[0, :4] * math.nan]) for t, n in ((q, rows), (k, keys), (v, keys), (g, rows))]
+    out, lse = at.attention_fwd(*pk[:3], q_offsets=offs[0], k_offsets=offs[1])
+    grads = at.attention_bwd(*pk[:3], out, lse, pk[3], q_offsets=offs[0], k_offsets=offs[1])
+    for b, (i, j) in enumerate(zip((slice(0, 130), slice(0, 0), slice(130, 207)), (slice(0, 60), slice(60, 200), slice(200, 200)))):
+        r = ref.one(pk[0][i], pk[1][j], pk[2][j], D ** -0.5, dout=pk[3][i])
+        for name, t in (("dq", grads[0][i]), ("dk", grads[1][j]), ("dv", grads[2][j])):
+            ref.check("%s of sequence %d" % (name, b), t, *r[name])
+    assert not grads[1][200:].any() and not grads[2][200:].any()
+    only = at.attention_bwd(*pk[:3], out, lse, pk[3], q_offsets=offs[0], k_offsets=offs[1], want=(False, False, True))
+    assert torch.equal(only[2], grads[2])
 
 
 def test_packed_rows_of_few_keys_and_many(at):
