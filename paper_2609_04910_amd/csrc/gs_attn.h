@@ -79,22 +79,40 @@ __device__ __forceinline__ AttnSeq seq_of(const AttnShape& s, int b) {
   return r;
 }
 
-// Tile `slot` of the packed rows: its sequence and its index within it.  The
-// tiles of all sequences (ceil(n * per / tile) each) are counted by one wave scan
-// of the offsets, 64 sequences a step.  Returns kNoRow where there is none, t then
-// being the number of tiles.
+// For each lane its sequence's place by descending key (equal keys by number), B at
+// most 64 sequences, one a lane.
+__device__ __forceinline__ int place_by(int key, int B) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < B ? clampi(key, 0, (1 << 25) - 1) << 6 | (63 - lane) : -1;
+  int place = 0;
+#pragma unroll 8
+  for (int b = 0; b < B; ++b) place += __builtin_amdgcn_readlane(mine, b) > mine;
+  return place;
+}
+
+// Tile `slot` of the packed rows: its sequence b, its index t within it and the
+// sequence's number n of tiles (ceil(rows * per / tile)).  The tiles of all sequences
+// are counted by one wave scan of the offsets, 64 sequences a step, up to 64
+// sequences in descending order of `keys` (NULL: of their rows), so that the long
+// ones start first.  Returns kNoRow where there is none, t then being the number of
+// all tiles.
 __device__ __forceinline__ int packed_tile(const int32_t* off, int B, int rows, int per, int tile, int slot,
-                                           int& t) {
+                                           const int32_t* keys, int& t, int& n) {
   const int lane = threadIdx.x & 63;
   int base = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
-    int n = 0;
-    if (b0 + lane < B) {
-      const int e0 = clampi(off[b0 + lane], 0, rows);
-      n = clampi(off[b0 + lane + 1], e0, rows) - e0;
-      n = (int)(((int64_t)n * per + tile - 1) / tile);
+    int m = 0, seq = b0 + lane;
+    if (seq < B) {
+      const int e0 = clampi(off[seq], 0, rows);
+      m = clampi(off[seq + 1], e0, rows) - e0;
+      m = (int)(((int64_t)m * per + tile - 1) / tile);
     }
-    int end = n;
+    if (B <= 64) {
+      seq = __builtin_amdgcn_ds_permute(place_by(keys && lane < B ? keys[lane] : m, B) * 4, lane);
+      m = __shfl(m, seq & 63);
+      if (lane >= B) m = 0;
+    }
+    int end = m;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int x = __shfl_up(end, d);
@@ -103,8 +121,9 @@ __device__ __forceinline__ int packed_tile(const int32_t* off, int B, int rows, 
     const uint64_t hit = __ballot(slot - base < end);
     if (hit) {
       const int w = __builtin_ctzll(hit);
-      t = slot - base - __builtin_amdgcn_readlane(end - n, w);
-      return b0 + w;
+      n = __builtin_amdgcn_readlane(m, w);
+      t = slot - base - (__builtin_amdgcn_readlane(end, w) - n);
+      return __builtin_amdgcn_readlane(seq, w);
     }
     base += __builtin_amdgcn_readlane(end, 63);
   }

@@ -197,8 +197,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
   block_place(blockIdx.x - split * a.wgs, a.heads, a.tiles, tile, head);
   const int rows_all = KV ? s.N : s.M;
   if (s.packed) {
-    const int slot = KV ? tile : a.tiles - 1 - tile;
-    b = packed_tile(KV ? s.k_index : s.q_index, s.B, rows_all, 1, COLS, slot, tile);
+    const int slot = tile;
+    int n;
+    b = packed_tile(KV ? s.k_index : s.q_index, s.B, rows_all, 1, COLS, slot, nullptr, tile, n);
     if (b == kNoRow) {
       if ((s.zero_rest & kRestOut) && split == 0) {
         const int part = slot - tile, parts = a.tiles - tile;
@@ -213,6 +214,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       }
       return;
     }
+    if (!KV) tile = n - 1 - tile;  // causal: late queries and early keys have most pairs
   } else {
     const int per_seq = a.heads / s.B;
     b = head / per_seq;

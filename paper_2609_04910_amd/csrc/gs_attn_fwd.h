@@ -225,18 +225,14 @@ struct AttnJob {
   int part;            // which split
 };
 
-// The sequence with the rank-th longest of B lengths (equal ones by number), so
-// that a batch's long sequences start first and its short ones fill in: 64
-// sequences of 2048 to 8192 keys, 8 key heads 333 -> 278 us (5.1 TB/s; equal lengths of 4096
-// 205 -> 211 us).  One lane a sequence;
-// more sequences than lanes even out by their number.
+// The sequence with the rank-th longest of B lengths, so that a batch's long
+// sequences start first and its short ones fill in: 64 sequences of 2048 to 8192
+// keys, 8 key heads 333 -> 278 us (5.1 TB/s; equal lengths of 4096 205 -> 211 us).
+// More sequences than lanes even out by their number.
 __device__ __forceinline__ int by_length(const int32_t* lens, int B, int rank) {
   if (B > 64) return rank;
   const int lane = threadIdx.x & 63;
-  const int mine = lane < B ? clampi(lens[lane], 0, (1 << 25) - 1) << 6 | (63 - lane) : -1;
-  int place = 0;
-#pragma unroll 8
-  for (int b = 0; b < B; ++b) place += __builtin_amdgcn_readlane(mine, b) > mine;
+  const int place = place_by(lane < B ? lens[lane] : 0, B);
   return __builtin_ctzll(__ballot(lane < B && place == rank));
 }
 
@@ -256,8 +252,9 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
   int tile, head;
   block_place(id, a.heads, a.tiles, tile, head);
   if (s.packed) {
-    const int slot = a.tiles - 1 - tile;
-    w.b = packed_tile(s.q_index, s.B, s.M, a.per, ROWS, slot, tile);
+    const int slot = tile;
+    int n;
+    w.b = packed_tile(s.q_index, s.B, s.M, a.per, ROWS, slot, PAGED ? a.pg.lens : nullptr, tile, n);
     if (w.b == kNoRow) {  // slots past the last tile: rows of no sequence
       if (s.zero_rest && w.part == 0) {
         const int part = slot - tile, parts = a.tiles - tile;
@@ -274,6 +271,7 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
       }
       return false;
     }
+    tile = n - 1 - tile;  // the tiles that see most keys first
   } else {
     const int per_seq = a.heads / s.B;
     if (SORT) {
