@@ -25,7 +25,10 @@ Rows that belong to no sequence are 0 (lse: -inf) in results allocated here and
 left as they were in the caller's own (out=, lse=).
 """
 import ctypes
+import functools
 import os
+import struct
+import threading
 
 from . import gauss_sum as gs
 
@@ -84,13 +87,34 @@ def load(path=LIB_PATH, torch_runtime=True):
     return lib
 
 
-def _array(t, packed):
+# The structures of a call are packed into one buffer a thread (a call reads them
+# before it returns): making them as ctypes objects takes longer than the call.
+_PROBLEM, _ARRAY, _CACHE = "8q4if4x", "4q", "13q"
+_AT_ARRAYS, _ARRAY_BYTES, _CACHE_BYTES = 88, 32, 104
+_PACK_FWD = struct.Struct("=" + _PROBLEM + 5 * _ARRAY).pack_into
+_PACK_BWD = struct.Struct("=" + _PROBLEM + 9 * _ARRAY).pack_into
+_PACK_PAGED = struct.Struct("=" + _PROBLEM + 2 * _ARRAY + _CACHE).pack_into
+_local = threading.local()
+
+
+def _buffer():
+    """(buffer, its address) of this thread."""
+    try:
+        return _local.buffer
+    except AttributeError:
+        buf = ctypes.create_string_buffer(_AT_ARRAYS + 9 * _ARRAY_BYTES + _CACHE_BYTES)
+        _local.buffer = buf, ctypes.addressof(buf)
+        return _local.buffer
+
+
+def _numbers(t, packed):
+    """The four numbers of a gs_attention_array (zeros: not given)."""
     if t is None:
-        return None
+        return 0, 0, 0, 0
     s = t.stride()
     if packed:
-        return Array(t.data_ptr(), 0, s[0], s[1])
-    return Array(t.data_ptr(), s[0], s[1], s[2])
+        return t.data_ptr(), 0, s[0], s[1]
+    return t.data_ptr(), s[0], s[1], s[2]
 
 
 def _check_columns(name, t, dims):
@@ -109,10 +133,6 @@ def _check_index(name, t, n, device):
                          % (name, "" if n is None else " of %d" % n, tuple(t.shape)))
     if t.device != device:
         raise ValueError("%s must be on %s" % (name, device))
-
-
-def _scale(scale, D):
-    return D ** -0.5 if scale is None else float(scale)
 
 
 def _dtype(*named):
@@ -135,59 +155,104 @@ def _check_gpu(*named):
             raise ValueError("%s must be on %s" % (name, device))
 
 
+def _check_call(q, k, v, causal, window, q_offsets, k_offsets, q_lens, k_lens):
+    """Refuses what a forward or backward call cannot take."""
+    packed = q_offsets is not None
+    if k_offsets is not None and not packed:
+        raise ValueError("k_offsets needs q_offsets")
+    if packed and (q_lens is not None or k_lens is not None):
+        raise ValueError("q_lens / k_lens are for dense sequences, q_offsets / k_offsets for packed ones")
+    dims = 3 if packed else 4
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        _check_columns(name, t, dims)
+    Hq, D = q.shape[-2:]
+    Hkv = v.shape[-2]
+    if k.shape[-2] != Hkv or k.shape[-1] != D or k.shape[:-2] != v.shape[:-2]:
+        raise ValueError("k must be %s (rows and heads of v, columns of q), got %s"
+                         % ("x".join(map(str, v.shape[:-1] + (D,))), tuple(k.shape)))
+    if Hkv < 1 or Hq % Hkv or Hq == 0:
+        raise ValueError("%d query heads over %d key heads: must be a multiple" % (Hq, Hkv))
+    if not packed and q.shape[0] != k.shape[0]:
+        raise ValueError("q has %d sequences, k has %d" % (q.shape[0], k.shape[0]))
+    if window < 0 or (window and not causal):
+        raise ValueError("window must be 0, or positive with causal")
+    _dtype(("q", q), ("k", k), ("v", v))
+    if packed:
+        _check_index("q_offsets", q_offsets, None, q.device)
+        if q_offsets.shape[0] < 1:
+            raise ValueError("q_offsets must hold one number more than there are sequences")
+        if k_offsets is not None:
+            _check_index("k_offsets", k_offsets, q_offsets.shape[0], q.device)
+    else:
+        for name, t in (("q_lens", q_lens), ("k_lens", k_lens)):
+            if t is not None:
+                _check_index(name, t, q.shape[0], q.device)
+    _check_gpu(("q", q), ("k", k), ("v", v))
+
+
 class _Call:
-    """Checked shapes of a forward or backward call."""
+    """Checked sizes of a forward or backward call."""
+    __slots__ = ("sizes", "modes", "scale", "packed", "index", "out_shape", "lse_shape", "gpu")
 
     def __init__(self, q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens):
-        packed = q_offsets is not None
-        if k_offsets is not None and not packed:
-            raise ValueError("k_offsets needs q_offsets")
-        if packed and (q_lens is not None or k_lens is not None):
-            raise ValueError("q_lens / k_lens are for dense sequences, q_offsets / k_offsets for packed ones")
-        dims = 3 if packed else 4
-        for name, t in (("q", q), ("k", k), ("v", v)):
-            _check_columns(name, t, dims)
-        Hq, D = q.shape[-2:]
-        Hkv, C = v.shape[-2:]
-        if k.shape[-2] != Hkv or k.shape[-1] != D or k.shape[:-2] != v.shape[:-2]:
-            raise ValueError("k must be %s (rows and heads of v, columns of q), got %s"
-                             % ("x".join(map(str, v.shape[:-1] + (D,))), tuple(k.shape)))
-        if Hkv < 1 or Hq % Hkv or Hq == 0:
-            raise ValueError("%d query heads over %d key heads: must be a multiple" % (Hq, Hkv))
-        if not packed and q.shape[0] != k.shape[0]:
-            raise ValueError("q has %d sequences, k has %d" % (q.shape[0], k.shape[0]))
-        if window < 0 or (window and not causal):
-            raise ValueError("window must be 0, or positive with causal")
-        code = _dtype(("q", q), ("k", k), ("v", v))
+        qs, ks, vs = q.shape, k.shape, v.shape
+        self.gpu = q.get_device()
+        # the usual call, told by its sizes alone; any other goes through the checks
+        if not (q_offsets is None and q_lens is None and k_lens is None and k_offsets is None
+                and len(qs) == 4 and len(vs) == 4 and window == 0 and ks == (qs[0], vs[1], vs[2], qs[3])
+                and vs[2] and qs[2] and qs[2] % vs[2] == 0 and vs[0] == qs[0]
+                and q.dtype in _dtypes() and k.dtype == q.dtype and v.dtype == q.dtype
+                and q.stride(3) == 1 and k.stride(3) == 1 and v.stride(3) == 1
+                and self.gpu >= 0 and k.get_device() == self.gpu and v.get_device() == self.gpu):
+            _check_call(q, k, v, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+        Hq, D = qs[-2:]
+        Hkv, C = vs[-2:]
+        self.packed = packed = q_offsets is not None
         if packed:
-            if k_offsets is None:
-                k_offsets = q_offsets
-            _check_index("q_offsets", q_offsets, None, q.device)
-            if q_offsets.shape[0] < 1:
-                raise ValueError("q_offsets must hold one number more than there are sequences")
-            _check_index("k_offsets", k_offsets, q_offsets.shape[0], q.device)
-            B, M, N = q_offsets.shape[0] - 1, q.shape[0], k.shape[0]
-            self.index = (q_offsets, k_offsets)
-            self.lse_shape = (Hq, M)
+            B, M, N = q_offsets.shape[0] - 1, qs[0], ks[0]
+            self.index = q_offsets, (q_offsets if k_offsets is None else k_offsets)
+            self.lse_shape = Hq, M
         else:
-            B, M, N = q.shape[0], q.shape[1], k.shape[1]
-            for name, t in (("q_lens", q_lens), ("k_lens", k_lens)):
-                if t is not None:
-                    _check_index(name, t, B, q.device)
-            self.index = (q_lens, k_lens)
-            self.lse_shape = (B, Hq, M)
-        _check_gpu(("q", q), ("k", k), ("v", v))
-        self.packed = packed
-        self.out_shape = q.shape[:-1] + (C,)
-        self.problem = Problem(B, M, N, Hq, Hkv, D, C, int(window), code, int(packed), int(bool(causal)), 0,
-                               _scale(scale, D))
+            B, M, N = qs[0], qs[1], ks[1]
+            self.index = q_lens, k_lens
+            self.lse_shape = B, Hq, M
+        self.out_shape = qs[:-1] + (C,)
+        self.sizes = B, M, N, Hq, Hkv, D, C, int(window)
+        self.modes = _dtypes()[q.dtype], int(packed), int(bool(causal))
+        self.scale = D ** -0.5 if scale is None else float(scale)
 
 
-def _launch(name, device, stream, *args):
-    """The library call on the tensors' device and the given (or its current) stream."""
+@functools.lru_cache(maxsize=None)
+def _dtypes():
     import torch
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
+    return {torch.float16: gs.GS_F16, torch.bfloat16: gs.GS_BF16}
+
+
+@functools.lru_cache(maxsize=4096)
+def _bwd_bytes(sizes, modes, want):
+    """Workspace of a backward call, by its sizes."""
+    p = Problem(*sizes, *modes, 0, 1.0)
+    return int(load().gs_attention_bwd_workspace_size(_ref(p), *want))
+
+
+@functools.lru_cache(maxsize=4096)
+def _fwd_bytes(sizes, modes):
+    p = Problem(*sizes, *modes, 0, 1.0)
+    return int(load().gs_attention_fwd_workspace_size(_ref(p)))
+
+
+@functools.lru_cache(maxsize=4096)
+def _paged_bytes(sizes, modes, page_size, table_width):
+    p = Problem(*sizes, *modes, 0, 1.0)
+    cache = Cache(Array(), Array(), 0, page_size, table_width, None, None)
+    return int(load().gs_attention_paged_workspace_size(_ref(p), _ref(cache)))
+
+
+def _launch(name, gpu, stream, *args):
+    """The library call on the tensors' GPU and the given (or its current) stream."""
+    import torch
+    if gpu != torch._C._cuda_getDevice():
+        with torch.cuda.device(gpu):
             st = getattr(load(), name)(*args, gs._stream(stream))
     else:
         st = getattr(load(), name)(*args, gs._stream(stream))
@@ -218,8 +283,6 @@ def _check_like_out(t, name, c, q):
 
 def _fwd(c, q, k, v, out, lse, low, workspace, stream):
     import torch
-    need = int(load().gs_attention_fwd_workspace_size(_ref(c.problem)))
-    workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
     rest = 0
     if out is None:
         rest = REST_OUT
@@ -231,12 +294,19 @@ def _fwd(c, q, k, v, out, lse, low, workspace, stream):
         rest |= REST_LSE
     else:
         gs._check_tensor(lse, "lse", c.lse_shape, q.device, torch.float32)
-    c.problem.zero_rest = rest
-    _launch("gs_attention_fwd", q.device, stream, _ref(c.problem), _ref(_array(q, c.packed)),
-            _ref(_array(k, c.packed)), _ref(_array(v, c.packed)), gs._ptr(c.index[0]), gs._ptr(c.index[1]),
-            _ref(_array(out, c.packed)), _ref(_array(low, c.packed)), gs._ptr(lse), gs._ptr(workspace),
-            wbytes)
-    gs._keep_alive(stream, out, lse, workspace)
+    need = _fwd_bytes(c.sizes, c.modes)
+    wbytes = 0
+    if need or workspace is not None:
+        workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
+    packed, index = c.packed, c.index
+    buf, at = _buffer()
+    _PACK_FWD(buf, 0, *c.sizes, *c.modes, rest, c.scale, *_numbers(q, packed), *_numbers(k, packed),
+              *_numbers(v, packed), *_numbers(out, packed), *_numbers(low, packed))
+    at += _AT_ARRAYS
+    _launch("gs_attention_fwd", c.gpu, stream, at - _AT_ARRAYS, at, at + 32, at + 64, gs._ptr(index[0]),
+            gs._ptr(index[1]), at + 96, None if low is None else at + 128, lse.data_ptr(), gs._ptr(workspace), wbytes)
+    if stream is not None:
+        gs._keep_alive(stream, out, lse, workspace)
     return out, lse
 
 
@@ -257,35 +327,36 @@ def attention_fwd(q, k, v, scale=None, causal=False, window=0, q_offsets=None, k
 
 def attention_fwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed=False):
     """Workspace bytes of attention_fwd (packed: M and N are the rows of all sequences)."""
-    p = Problem(B, M, N, Hq, Hkv, D, C, 0, dtype, int(packed), 0, 0, 1.0)
-    return int(load().gs_attention_fwd_workspace_size(_ref(p)))
+    return _fwd_bytes((B, M, N, Hq, Hkv, D, C, 0), (dtype, int(packed), 0))
 
 
-def attention_bwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed=False,
+def attention_bwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed=False, causal=False, window=0,
                                  want_dq=True, want_dk=True, want_dv=True):
     """Workspace bytes of attention_bwd (packed: M and N are the rows of all sequences)."""
-    p = Problem(B, M, N, Hq, Hkv, D, C, 0, dtype, int(packed), 0, 0, 1.0)
-    return int(load().gs_attention_bwd_workspace_size(_ref(p), int(bool(want_dq)), int(bool(want_dk)),
-                                                      int(bool(want_dv))))
+    return _bwd_bytes((B, M, N, Hq, Hkv, D, C, int(window)), (dtype, int(packed), int(bool(causal))),
+                      (int(bool(want_dq)), int(bool(want_dk)), int(bool(want_dv))))
 
 
 def _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream):
     import torch
-    for name, t in (("out", out), ("dout", dout), ("low", low)):
-        if name != "low" or t is not None:
-            _check_like_out(t, name, c, q)
-    gs._check_tensor(lse, "lse", c.lse_shape, q.device, torch.float32)
-    grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if w else None
-             for t, w in zip((q, k, v), want)]
-    c.problem.zero_rest = REST_OUT
-    need = int(load().gs_attention_bwd_workspace_size(_ref(c.problem), *(int(bool(w)) for w in want)))
-    workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
-    _launch("gs_attention_bwd", q.device, stream, _ref(c.problem), _ref(_array(q, c.packed)),
-            _ref(_array(k, c.packed)), _ref(_array(v, c.packed)), gs._ptr(c.index[0]), gs._ptr(c.index[1]),
-            _ref(_array(out, c.packed)), _ref(_array(low, c.packed)), gs._ptr(lse), _ref(_array(dout, c.packed)),
-            *(_ref(_array(g, c.packed)) for g in grads), gs._ptr(workspace), wbytes)
-    gs._keep_alive(stream, workspace, *grads)
-    return tuple(grads)
+    want = int(bool(want[0])), int(bool(want[1])), int(bool(want[2]))
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want[0] else None
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if want[1] else None
+    dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if want[2] else None
+    workspace, wbytes = gs._workspace_arg(workspace, _bwd_bytes(c.sizes, c.modes, want), q.device)
+    packed, index = c.packed, c.index
+    buf, at = _buffer()
+    _PACK_BWD(buf, 0, *c.sizes, *c.modes, REST_OUT, c.scale, *_numbers(q, packed), *_numbers(k, packed),
+              *_numbers(v, packed), *_numbers(out, packed), *_numbers(low, packed), *_numbers(dout, packed),
+              *_numbers(dq, packed), *_numbers(dk, packed), *_numbers(dv, packed))
+    at += _AT_ARRAYS
+    _launch("gs_attention_bwd", c.gpu, stream, at - _AT_ARRAYS, at, at + 32, at + 64, gs._ptr(index[0]),
+            gs._ptr(index[1]), at + 96, None if low is None else at + 128, lse.data_ptr(), at + 160,
+            at + 192 if want[0] else None, at + 224 if want[1] else None, at + 256 if want[2] else None,
+            gs._ptr(workspace), wbytes)
+    if stream is not None:
+        gs._keep_alive(stream, workspace, dq, dk, dv)
+    return dq, dk, dv
 
 
 def attention_bwd(q, k, v, out, lse, dout, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None,
@@ -293,7 +364,12 @@ def attention_bwd(q, k, v, out, lse, dout, scale=None, causal=False, window=0, q
     """(dq, dk, dv) of L = sum <dout, out> for the out, lse and (optional) low of attention_fwd with the
     same arguments; None where not wanted.  dk and dv are summed over the query heads that share a key
     head."""
+    import torch
     c = _Call(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+    for name, t in (("out", out), ("dout", dout), ("low", low)):
+        if name != "low" or t is not None:
+            _check_like_out(t, name, c, q)
+    gs._check_tensor(lse, "lse", c.lse_shape, q.device, torch.float32)
     return _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream)
 
 
@@ -314,8 +390,8 @@ def _make_autograd():
         def backward(ctx, g):
             q, k, v, out, lse, low = ctx.saved_tensors[:6]
             want = ctx.needs_input_grad[:3]
-            if not any(want):
-                return None, None, None, None
+            if g.dtype != q.dtype:
+                g = g.to(q.dtype)
             if g.shape[-1] > 1 and g.stride(-1) != 1:
                 g = g.contiguous()
             return _bwd(ctx.call, q, k, v, out, lse, g, want, low, None, None) + (None,)
@@ -335,8 +411,8 @@ def attention(q, k, v, scale=None, causal=False, window=0, q_offsets=None, k_off
     return _autograd.apply(q, k, v, c)
 
 
-def _cache_call(x, name, k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window, scale):
-    """(problem, cache, packed) of a call on T x H x width rows x."""
+def _cache_call(x, name, k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window):
+    """Checked (sizes, modes) of a call on T x H x width rows x."""
     import torch
     for n, t in (("k_pages", k_pages), ("v_pages", v_pages)):
         _check_columns(n, t, 4)
@@ -365,16 +441,20 @@ def _cache_call(x, name, k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, 
         M = T // B if B else 0
     if window < 0:
         raise ValueError("window must not be negative")
-    p = Problem(B, M, 0, Hq, Hkv, D, C, int(window), code, int(q_offsets is not None), 1, 0, scale)
-    cache = Cache(_array(k_pages, False), _array(v_pages, False), k_pages.shape[0], k_pages.shape[1],
-                  page_table.shape[1], page_table.data_ptr(), seq_lens.data_ptr())
-    return p, cache
+    sizes = B, M, 0, Hq, Hkv, D, C, int(window)
+    return sizes, (code, int(q_offsets is not None), 1)
 
 
-def _rows(t, p):
+def _cache_numbers(k_pages, v_pages, page_table, seq_lens):
+    """The thirteen numbers of a gs_attention_cache."""
+    return (*_numbers(k_pages, False), *_numbers(v_pages, False), k_pages.shape[0], k_pages.shape[1],
+            page_table.shape[1], page_table.data_ptr(), seq_lens.data_ptr())
+
+
+def _row_numbers(t, sizes, modes):
     """T x H x width rows: packed, or M of every sequence."""
     s = t.stride()
-    return Array(t.data_ptr(), 0 if p.packed else p.M * s[0], s[0], s[1])
+    return t.data_ptr(), 0 if modes[1] else sizes[1] * s[0], s[0], s[1]
 
 
 def attention_append(k, v, k_pages, v_pages, page_table, seq_lens, q_offsets=None, stream=None):
@@ -390,20 +470,20 @@ def attention_append(k, v, k_pages, v_pages, page_table, seq_lens, q_offsets=Non
         raise ValueError("k and v must share rows and heads, got %s and %s" % (tuple(k.shape), tuple(v.shape)))
     code = _dtype(("k", k), ("v", v), ("k_pages", k_pages), ("v_pages", v_pages))
     H = k.shape[1]
-    p, cache = _cache_call(k, "k", k_pages, v_pages, page_table, seq_lens, q_offsets, H, k.shape[2], v.shape[2],
-                           code, 0, 1.0)
-    if p.Hkv != H:
-        raise ValueError("k has %d heads, the pages have %d" % (H, p.Hkv))
+    sizes, modes = _cache_call(k, "k", k_pages, v_pages, page_table, seq_lens, q_offsets, H, k.shape[2], v.shape[2],
+                               code, 0)
+    if sizes[4] != H:
+        raise ValueError("k has %d heads, the pages have %d" % (H, sizes[4]))
     _check_gpu(("k", k), ("v", v), ("k_pages", k_pages), ("v_pages", v_pages))
-    _launch("gs_attention_append", k.device, stream, _ref(p), _ref(_rows(k, p)), _ref(_rows(v, p)), _ref(cache),
-            gs._ptr(q_offsets))
+    buf, at = _buffer()
+    _PACK_PAGED(buf, 0, *sizes, *modes, 0, 1.0, *_row_numbers(k, sizes, modes), *_row_numbers(v, sizes, modes),
+                *_cache_numbers(k_pages, v_pages, page_table, seq_lens))
+    _launch("gs_attention_append", k.get_device(), stream, at, at + 88, at + 120, at + 152, gs._ptr(q_offsets))
 
 
 def attention_paged_workspace_size(B, M, Hq, Hkv, D, C, page_size, table_width, dtype=gs.GS_F16, packed=False):
     """Workspace bytes of attention_paged (M: tokens of a sequence; packed: of all sequences)."""
-    p = Problem(B, M, 0, Hq, Hkv, D, C, 0, dtype, int(packed), 1, 0, 1.0)
-    cache = Cache(Array(), Array(), 0, page_size, table_width, None, None)
-    return int(load().gs_attention_paged_workspace_size(_ref(p), _ref(cache)))
+    return _paged_bytes((B, M, 0, Hq, Hkv, D, C, 0), (dtype, int(packed), 1), page_size, table_width)
 
 
 def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, scale=None, window=0, out=None,
@@ -420,11 +500,11 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     code = _dtype(("q", q), ("k_pages", k_pages), ("v_pages", v_pages))
     T, Hq, D = q.shape
     C = v_pages.shape[3]
-    p, cache = _cache_call(q, "q", k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window,
-                           _scale(scale, D))
+    sizes, modes = _cache_call(q, "q", k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window)
     _check_gpu(("q", q), ("k_pages", k_pages), ("v_pages", v_pages))
+    rest = 0
     if out is None:
-        p.zero_rest = REST_OUT
+        rest = REST_OUT
         out = torch.empty((T, Hq, C), dtype=q.dtype, device=q.device)
     else:
         _check_out(out, "out", (T, Hq, C), q.dtype, q.device)
@@ -432,10 +512,17 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     lse = None
     if return_lse:
         lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
-        p.zero_rest |= REST_LSE
-    need = int(load().gs_attention_paged_workspace_size(_ref(p), _ref(cache)))
-    workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
-    _launch("gs_attention_paged", q.device, stream, _ref(p), _ref(_rows(q, p)), _ref(cache), gs._ptr(q_offsets),
-            _ref(_rows(out, p)), gs._ptr(lse), gs._ptr(workspace), wbytes)
-    gs._keep_alive(stream, out, lse, workspace)
+        rest |= REST_LSE
+    need = _paged_bytes(sizes, modes, k_pages.shape[1], page_table.shape[1])
+    wbytes = 0
+    if need or workspace is not None:
+        workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
+    buf, at = _buffer()
+    _PACK_PAGED(buf, 0, *sizes, *modes, rest, D ** -0.5 if scale is None else float(scale),
+                *_row_numbers(q, sizes, modes), *_row_numbers(out, sizes, modes),
+                *_cache_numbers(k_pages, v_pages, page_table, seq_lens))
+    _launch("gs_attention_paged", q.get_device(), stream, at, at + 88, at + 152, gs._ptr(q_offsets), at + 120,
+            gs._ptr(lse), gs._ptr(workspace), wbytes)
+    if stream is not None:
+        gs._keep_alive(stream, out, lse, workspace)
     return (out, lse) if return_lse else out

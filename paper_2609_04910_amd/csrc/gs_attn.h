@@ -17,8 +17,7 @@
 // (16 bytes a lane) where rows are 16-byte aligned and a multiple of 8 wide, and
 // element by element otherwise.  A tile row is DP 16-bit elements (DP = 64, 128
 // or 256, columns past the caller's width zero); its 16-byte chunk c lies at
-// chunk c ^ swz(row), so the row reads (eight rows, one chunk) and the
-// transposing reads (four rows, two chunks) both spread over the banks.
+// chunk c ^ swz(row), so that the operand reads spread over the LDS banks.
 #pragma once
 
 #include "gs_common.h"
@@ -241,6 +240,9 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// The XOR of a row's chunks: the row reads (eight rows, one chunk) and the
+// transposing reads (four rows, two chunks) spread over the banks.  (A swizzle
+// that spreads 16 rows over 256 bytes measured the same, with more registers.)
 __host__ __device__ constexpr int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
 
 // A value that is the same in all lanes, in a scalar register.
@@ -360,68 +362,31 @@ __device__ __forceinline__ uint4 tr_operand(const char* tile, const TileLane<DP>
 // D = 128 kernels then spilled 50 to 450 values inside the tile loop).
 __device__ __forceinline__ void stage_fence() { __builtin_amdgcn_sched_barrier(0x6); }
 
-// Operands are read kAhead stages before the matrix instructions that use them.
-constexpr int kAhead = 2;
-
-// s[n] += X U[n] over NC chunks of 32 columns: rows 16 t .. of a tile.
-template <typename T, int DP, int NT>
-__device__ __forceinline__ void scores(const char* tile, const TileLane<DP>& ln, int t, const uint4 (&u)[NT][DP / 32],
-                                       floatx4 (&s)[NT]) {
-  constexpr int NC = DP / 32, P = kAhead < NC ? kAhead : NC - 1;
+// N stages of a contraction: operand i is read P stages before use(i, operand), the
+// first P of them before the first stage (preload), and the last stages read the
+// first operands of what comes next (into `next`), so that no phase begins with a
+// wait for LDS.  The loops unroll: i is a constant in load and use.
+template <int P>
+struct Ahead {
   uint4 x[P + 1];
+  template <typename Load>
+  __device__ __forceinline__ void preload(Load load) {
 #pragma unroll
-  for (int c = 0; c < P; ++c) x[c] = row_operand<DP>(tile, ln, t, c);
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    if (c + P < NC) x[(c + P) % (P + 1)] = row_operand<DP>(tile, ln, t, c + P);
-    stage_fence();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) s[n] = mfma_qk<T>(x[c % (P + 1)], u[n][c], s[n]);
-    stage_fence();
+    for (int i = 0; i < P; ++i) x[i] = load(i);
   }
-}
-
-// d[t][n] += Y W[n] for the two row tiles of step s, with the column operands W
-// read from LDS as well (rows 16 n .. of `cols`).
-template <typename T, int DP, int NT>
-__device__ __forceinline__ void scores_lds(const char* tile, const char* cols, const TileLane<DP>& ln, int s,
-                                           floatx4 (&d)[2][NT]) {
-  constexpr int NC = DP / 32;
-  uint4 y[2][2], w[2][NT];
-  auto read = [&](int c) {
+};
+struct NoLoad {};
+template <int N, int P, typename Load, typename Use, typename Next>
+__device__ __forceinline__ void stages(Ahead<P>& ops, Load load, Use use, Ahead<P>& next, Next next_load) {
+  static_assert(N >= P, "stages");
 #pragma unroll
-    for (int n = 0; n < NT; ++n) w[c & 1][n] = row_operand<DP>(cols, ln, n, c);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) y[c & 1][t] = row_operand<DP>(tile, ln, 2 * s + t, c);
-  };
-  read(0);
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    if (c + 1 < NC) read(c + 1);
+  for (int i = 0; i < N; ++i) {
+    if (i + P < N)
+      ops.x[(i + P) % (P + 1)] = load(i + P);
+    else if constexpr (!__is_same(Next, NoLoad))
+      next.x[i + P - N] = next_load(i + P - N);
     stage_fence();
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) d[t][n] = mfma_qk<T>(y[c & 1][t], w[c & 1][n], d[t][n]);
-    stage_fence();
-  }
-}
-
-// acc[ct][n] += X^T B[n] over the 32 rows of step s of a tile: NC transposed
-// operands, NT column tiles.
-template <typename T, int DP, int NC, int NT>
-__device__ __forceinline__ void contract(const char* tile, const TileLane<DP>& ln, int s, const uint4 (&b)[NT],
-                                         floatx4 (&acc)[NC][NT]) {
-  constexpr int P = kAhead < NC ? kAhead : NC - 1;
-  uint4 a[P + 1];
-#pragma unroll
-  for (int ct = 0; ct < P; ++ct) a[ct] = tr_operand<DP>(tile, ln, s, ct);
-#pragma unroll
-  for (int ct = 0; ct < NC; ++ct) {
-    if (ct + P < NC) a[(ct + P) % (P + 1)] = tr_operand<DP>(tile, ln, s, ct + P);
-    stage_fence();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[ct][n] = mfma_qk<T>(a[ct % (P + 1)], b[n], acc[ct][n]);
+    use(i, ops.x[i % (P + 1)]);
     stage_fence();
   }
 }

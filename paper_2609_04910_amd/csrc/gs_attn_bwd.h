@@ -364,10 +364,41 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
             dp2[t][n] = KV ? -*reinterpret_cast<const floatx4*>(&stat[stage][1][32 * hf + 16 * t + 4 * g])
                            : floatx4{-cdelta[n], -cdelta[n], -cdelta[n], -cdelta[n]};
           }
+        Ahead<2> xo, yo;
+        auto load_x = [&](int t, int c) { return row_operand<DP>(xt, ln, 2 * hf + t, c); };
+        auto load_y = [&](int t, int c) { return row_operand<DP>(yt, ln, 2 * hf + t, c); };
+        auto load_ytr = [&](int i) { return tr_operand<DP>(yt, ln, hf, i); };
+        auto load_xtr = [&](int i) { return tr_operand<DP>(xt, ln, hf, i); };
+        xo.preload([&](int i) { return load_x(0, i); });
         if constexpr (WLDS) {
+          // S of both row tiles, then dP with the operands of V from LDS
+          stages<2 * NC>(
+              xo, [&](int i) { return load_x(i / NC, i % NC); },
+              [&](int i, const uint4& x) {
 #pragma unroll
-          for (int t = 0; t < 2; ++t) scores<T, DP, NT>(xt, ln, 2 * hf + t, uo, sc2[t]);
-          scores_lds<T, DP, NT>(yt, wmine, ln, hf, dp2);
+                for (int n = 0; n < NT; ++n) sc2[i / NC][n] = mfma_qk<T>(x, uo[n][i % NC], sc2[i / NC][n]);
+              },
+              yo, NoLoad{});
+          uint4 y[2][2], w[2][NT];
+          auto read = [&](int c) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) w[c & 1][n] = row_operand<DP>(wmine, ln, n, c);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) y[c & 1][t] = load_y(t, c);
+          };
+          read(0);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            if (c + 1 < NC) read(c + 1);
+            stage_fence();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int n = 0; n < NT; ++n) dp2[t][n] = mfma_qk<T>(y[c & 1][t], w[c & 1][n], dp2[t][n]);
+            stage_fence();
+          }
+          yo.preload(load_ytr);
+          stage_fence();
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -375,8 +406,22 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
           floatx4 rl{0, 0, 0, 0};
           if (KV) rl = *reinterpret_cast<const floatx4*>(&stat[stage][0][32 * hf + 16 * t + 4 * g]);
           if constexpr (!WLDS) {
-            scores<T, DP, NT>(xt, ln, 2 * hf + t, uo, sc);
-            scores<T, DP, NT>(yt, ln, 2 * hf + t, wo, dp);
+            stages<NC>(
+                xo, [&](int i) { return load_x(t, i); },
+                [&](int i, const uint4& x) {
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) sc[n] = mfma_qk<T>(x, uo[n][i], sc[n]);
+                },
+                yo, [&](int i) { return load_y(t, i); });
+            // what is read ahead of the exponentials: the next row tile's rows, or the
+            // first transposed operands (of dO for dV, of K for dQ)
+            stages<NC>(
+                yo, [&](int i) { return load_y(t, i); },
+                [&](int i, const uint4& y) {
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) dp[n] = mfma_qk<T>(y, wo[WLDS ? 0 : n][i], dp[n]);
+                },
+                xo, [&](int i) { return t == 0 ? load_x(1, i) : KV ? load_ytr(i) : load_xtr(i); });
           }
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -406,8 +451,22 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
           pb[n] = uint4{pw[n][0], pw[n][1], pw[n][2], pw[n][3]};
           db[n] = uint4{dsw[n][0], dsw[n][1], dsw[n][2], dsw[n][3]};
         }
-        if constexpr (KV) contract<T, DP>(yt, ln, hf, pb, dw);
-        contract<T, DP>(xt, ln, hf, db, du);
+        Ahead<2>& first = WLDS ? yo : xo;
+        if constexpr (KV)
+          stages<NO>(
+              first, load_ytr,
+              [&](int i, const uint4& y) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) dw[KV ? i : 0][n] = mfma_qk<T>(y, pb[n], dw[KV ? i : 0][n]);
+              },
+              WLDS ? xo : yo, load_xtr);
+        stages<NO>(
+            KV && !WLDS ? yo : xo, load_xtr,
+            [&](int i, const uint4& x) {
+#pragma unroll
+              for (int n = 0; n < NT; ++n) du[i][n] = mfma_qk<T>(x, db[n], du[i][n]);
+            },
+            first, NoLoad{});
       }
     }
 

@@ -89,8 +89,10 @@ struct PageSlice {
 template <int DP>
 constexpr int attn_keys() { return DP == 256 ? 32 : 64; }
 
-template <int DP>
+template <int DP, bool PAGED>
 constexpr int attn_stages() { return 2; }
+template <int DP, bool PAGED>
+constexpr int attn_tile() { return attn_keys<DP>(); }
 
 // Query operand: columns 32c + 8g .. +7 of one row, zero past the width.
 template <typename T>
@@ -362,18 +364,42 @@ struct AttnRows {
     }
   }
 
-  // The 32 keys key0 .. of step h of a tile.  masked: some row does not see all
-  // of them; bad: some of them may lie on a page outside the cache.
+  // The keys key0 .. of a tile, H steps of 32.  masked: some row does not see all
+  // of them; pages->bad: some of them may lie on a page outside the cache.
+  template <int H>
   __device__ __forceinline__ void attend(const AttnFwdArgs& a, const char* kt, const char* vt, const TileLane<DP>& ln,
-                                         int h, int key0, bool masked, const PageSlice* pages) {
-    const int g = (threadIdx.x & 63) >> 4;
-    floatx4 x[2][NQ];
+                                         int key0, bool masked, const PageSlice* pages) {
+    // one stage ahead at D = 128 with three row tiles (two spill), else two
+    Ahead<DP == 128 && NQ == 3 ? 1 : 2> ko, vo;
+    ko.preload([&](int i) { return row_operand<DP>(kt, ln, i / NC, i % NC); });
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int h = 0; h < H; ++h) {
+      floatx4 x[2][NQ];
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) x[t][n] = floatx4{0, 0, 0, 0};
-      scores<T, DP, NQ>(kt, ln, 2 * h + t, q, x[t]);
+      for (int n = 0; n < NQ; ++n) x[0][n] = x[1][n] = floatx4{0, 0, 0, 0};
+      stages<2 * NC>(
+          ko, [&](int i) { return row_operand<DP>(kt, ln, 2 * h + i / NC, i % NC); },
+          [&](int i, const uint4& k) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) x[i / NC][n] = mfma_qk<T>(k, q[n][i % NC], x[i / NC][n]);
+          },
+          vo, [&](int i) { return tr_operand<DP>(vt, ln, h, i); });
+      uint4 w[NQ];
+      weights(a, key0 + 32 * h, masked, pages, x, w);
+      stages<NO>(
+          vo, [&](int i) { return tr_operand<DP>(vt, ln, h, i); },
+          [&](int i, const uint4& v) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) o[i][n] = mfma_qk<T>(v, w[n], o[i][n]);
+          },
+          ko, [&](int i) { return h + 1 < H ? row_operand<DP>(kt, ln, 2 * h + 2 + i / NC, i % NC) : uint4{}; });
     }
+  }
+
+  // Scores x of 32 keys to weights w, the offsets and sums brought up to date.
+  __device__ __forceinline__ void weights(const AttnFwdArgs& a, int key0, bool masked, const PageSlice* pages,
+                                          floatx4 (&x)[2][NQ], uint4 (&w)[NQ]) {
+    const int g = (threadIdx.x & 63) >> 4;
     if (masked || (pages && pages->bad)) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -388,7 +414,6 @@ struct AttnRows {
           }
         }
     }
-    uint4 w[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       float mx = x[0][n][0];
@@ -421,7 +446,6 @@ struct AttnRows {
       w[n] = uint4{pack2<T>(x[0][n][0], x[0][n][1]), pack2<T>(x[0][n][2], x[0][n][3]),
                    pack2<T>(x[1][n][0], x[1][n][1]), pack2<T>(x[1][n][2], x[1][n][3])};
     }
-    contract<T, DP>(vt, ln, h, w, o);
   }
   int max_key;  // the last key whose page number is at hand
 };
@@ -463,7 +487,7 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
 
 template <typename T, int DP, int NQ, int NW, bool PAGED, bool WIDE>
 __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
-  constexpr int BK = attn_keys<DP>(), NS = attn_stages<DP>(), NO = DP / 16, TILE = BK * DP * 2, ROWS = 16 * NQ * NW;
+  constexpr int BK = attn_tile<DP, PAGED>(), NS = attn_stages<DP, PAGED>(), NO = DP / 16, TILE = BK * DP * 2, ROWS = 16 * NQ * NW;
   constexpr int NB = (NO * 4 + 31) / 32;
   __shared__ __align__(1024) char smem[NS * 2 * TILE];
   __shared__ int mark[4];
@@ -542,9 +566,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
       if (key0 < mine.hi && key0 + BK > mine.lo) {
         const char* kt = smem + stage * 2 * TILE;
         const bool masked = key0 + BK > mine.in_hi || key0 < mine.in_lo;
-#pragma unroll
-        for (int h = 0; h < BK / 32; ++h)
-          rows.attend(a, kt, kt + TILE, ln, h, key0 + 32 * h, masked, PAGED ? &pages : nullptr);
+        rows.template attend<BK / 32>(a, kt, kt + TILE, ln, key0, masked, PAGED ? &pages : nullptr);
       }
       stage = stage + 1 == NS ? 0 : stage + 1;
     }
@@ -636,7 +658,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
                                                !infinities);
         infinities = true;
       }
-      rows.attend(a, kt, kt + TILE, ln, 0, key0, masked, PAGED ? &pages : nullptr);
+      rows.template attend<1>(a, kt, kt + TILE, ln, key0, masked, PAGED ? &pages : nullptr);
     }
     from = to;
   }
