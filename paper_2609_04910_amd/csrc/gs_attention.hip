@@ -580,8 +580,7 @@ gs_status run_append(const gs_attention_problem* p, const gs_attention_array* k,
   if (cache->table_width == 0 || cache->pages == 0) return GS_SUCCESS;
   a.s = shape_of(*p, q_index, nullptr);
   a.chunks = (int32_t)(((p->D > p->C ? p->D : p->C) + 7) / 8);
-  a.units = B * p->M * p->Hkv * a.chunks;
-  const int64_t grid = (a.units + 255) / 256;
+  const int64_t grid = (B * p->M + 3) / 4;
   if (grid > kMaxGrid) return GS_ERR_BAD_SHAPE;
   return launch(&k_attn_append, grid, 256, a, stream) == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
 }

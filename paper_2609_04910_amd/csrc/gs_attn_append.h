@@ -1,7 +1,8 @@
 // gs_attn_append.h -- keys and values of new tokens written to their places in the
 // pages of a cache: token i of the qn new ones of a sequence of length L (new
-// ones included) goes to position L - qn + i.  Bound by memory traffic: one thread
-// moves 16 bytes (or single elements where rows are not 16-byte aligned).
+// ones included) goes to position L - qn + i.  Bound by memory traffic: a wave
+// takes a token, looks its place up once in scalar registers, and moves 16 bytes a
+// lane (or single elements where rows are not 16-byte aligned).
 #pragma once
 
 #include "gs_attn_fwd.h"
@@ -13,8 +14,7 @@ struct AttnAppendArgs {
   AttnArray k, v;        // new tokens: row stride sr, head stride sh
   AttnArray kp, vp;      // pages: row stride sr, head stride sh
   AttnPages pg;
-  int64_t units;         // rows x key heads x chunks of the wider of K and V
-  int32_t chunks;
+  int32_t chunks;        // 16-byte chunks of the wider of a row of K and one of V
 };
 
 __device__ __forceinline__ void move_chunk(const AttnArray& src, const AttnArray& dst, const char* from, char* to,
@@ -29,12 +29,9 @@ __device__ __forceinline__ void move_chunk(const AttnArray& src, const AttnArray
 
 __global__ __launch_bounds__(256) void k_attn_append(const AttnAppendArgs a) {
   const AttnShape& s = a.s;
-  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (unit >= a.units) return;
-  const int c = (int)(unit % a.chunks);
-  const int64_t rest = unit / a.chunks;
-  const int h = (int)(rest % s.Hkv);
-  const int64_t row = rest / s.Hkv;  // over all sequences
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // over all sequences
+  if (row >= (int64_t)(s.packed ? 1 : s.B) * s.M) return;
   int b, i, qn;
   if (s.packed) {
     int l = 0, r = s.B;  // the last sequence that starts at or before the row
@@ -61,10 +58,15 @@ __global__ __launch_bounds__(256) void k_attn_append(const AttnAppendArgs a) {
   const int page = a.pg.table[(int64_t)b * a.pg.width + pi];
   if ((uint32_t)page >= (uint32_t)a.pg.pages) return;
   const int64_t sq = s.packed ? 0 : b, at_row = s.packed ? row : i;
-  move_chunk(a.k, a.kp, a.k.p + sq * a.k.sb + at_row * a.k.sr + h * a.k.sh,
-             a.kp.p + page * a.pg.page_stride_k + at * a.kp.sr + h * a.kp.sh, c, s.D);
-  move_chunk(a.v, a.vp, a.v.p + sq * a.v.sb + at_row * a.v.sr + h * a.v.sh,
-             a.vp.p + page * a.pg.page_stride_v + at * a.vp.sr + h * a.vp.sh, c, s.C);
+  const char* k = a.k.p + sq * a.k.sb + at_row * a.k.sr;
+  const char* v = a.v.p + sq * a.v.sb + at_row * a.v.sr;
+  char* kp = a.kp.p + page * a.pg.page_stride_k + at * a.kp.sr;
+  char* vp = a.vp.p + page * a.pg.page_stride_v + at * a.vp.sr;
+  for (int j = lane; j < s.Hkv * a.chunks; j += 64) {
+    const int h = j / a.chunks, c = j - h * a.chunks;
+    move_chunk(a.k, a.kp, k + h * a.k.sh, kp + h * a.kp.sh, c, s.D);
+    move_chunk(a.v, a.vp, v + h * a.v.sh, vp + h * a.vp.sh, c, s.C);
+  }
 }
 
 }  // namespace gs
