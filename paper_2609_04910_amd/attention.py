@@ -251,11 +251,12 @@ def _paged_bytes(sizes, modes, page_size, table_width):
 def _launch(name, gpu, stream, *args):
     """The library call on the tensors' GPU and the given (or its current) stream."""
     import torch
-    if gpu != torch._C._cuda_getDevice():
-        with torch.cuda.device(gpu):
-            st = getattr(load(), name)(*args, gs._stream(stream))
+    call = getattr(_lib or load(), name)
+    if gpu == torch._C._cuda_getDevice():
+        st = call(*args, torch._C._cuda_getCurrentRawStream(gpu) if stream is None else stream.cuda_stream)
     else:
-        st = getattr(load(), name)(*args, gs._stream(stream))
+        with torch.cuda.device(gpu):
+            st = call(*args, gs._stream(stream))
     if st != 0:
         raise gs.GaussSumError(st, name)
 
@@ -386,16 +387,20 @@ def _make_autograd():
             return out
 
         @staticmethod
-        @torch.autograd.function.once_differentiable
         def backward(ctx, g):
-            q, k, v, out, lse, low = ctx.saved_tensors[:6]
-            want = ctx.needs_input_grad[:3]
-            if g.dtype != q.dtype:
-                g = g.to(q.dtype)
-            if g.shape[-1] > 1 and g.stride(-1) != 1:
-                g = g.contiguous()
-            return _bwd(ctx.call, q, k, v, out, lse, g, want, low, None, None) + (None,)
+            # with create_graph the gradients are marked as not differentiable again;
+            # the wrapper that does so takes 20 us, so other calls go without
+            return (marked if torch.is_grad_enabled() else gradients)(ctx, g)
 
+    def gradients(ctx, g):
+        q, k, v, out, lse, low = ctx.saved_tensors[:6]
+        if g.dtype != q.dtype:
+            g = g.to(q.dtype)
+        if g.shape[-1] > 1 and g.stride(-1) != 1:
+            g = g.contiguous()
+        return _bwd(ctx.call, q, k, v, out, lse, g, ctx.needs_input_grad[:3], low, None, None) + (None,)
+
+    marked = torch.autograd.function.once_differentiable(gradients)
     return Attention
 
 

@@ -17,7 +17,7 @@ namespace gs {
 
 // At most this many workgroups of the preparation look at norms; each writes its
 // own maximum, and the passes take the largest (no atomics, nothing to clear).
-constexpr int kNormBlocks = 256;
+constexpr int kNormBlocks = 512;
 
 struct AttnBwdArgs {
   AttnShape s;
@@ -44,18 +44,24 @@ template <typename T>
 constexpr bool scaled() { return __is_same(T, F16); }
 
 __device__ __forceinline__ int ds_exponent(const float* norms, int q_blocks, int k_blocks) {
+  // all loads at once, then their maximum
+  float x[2][kNormBlocks / 64];
+#pragma unroll
+  for (int i = 0; i < kNormBlocks / 64; ++i) {
+    const int at = i * 64 + (threadIdx.x & 63);
+    x[0][i] = at < q_blocks ? norms[at] : 0.0f;
+    x[1][i] = at < k_blocks ? norms[kNormBlocks + at] : 0.0f;
+  }
   float z = 1.0f;
+#pragma unroll
   for (int side = 0; side < 2; ++side) {
     float m = 0.0f;
-    const int n = side ? k_blocks : q_blocks;
-    for (int i = threadIdx.x & 63; i < n; i += 64) {
-      const float x = norms[side * kNormBlocks + i];
-      m = x <= m ? m : x;
-    }
+#pragma unroll
+    for (int i = 0; i < kNormBlocks / 64; ++i) m = x[side][i] <= m ? m : x[side][i];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const float x = __shfl_xor(m, d);
-      m = x <= m ? m : x;
+      const float y = __shfl_xor(m, d);
+      m = y <= m ? m : y;
     }
     z *= m;
   }

@@ -333,6 +333,17 @@ def test_hidden_infinities_reach_no_gradient(at, dtype):
     assert dk[0, :31].isfinite().all() and dv[0, 110:].isfinite().all()
 
 
+def test_second_derivatives_are_refused(at):
+    """create_graph: the first gradients as ever, and an error, not a wrong value, for the second."""
+    q, k, v, g = make(25, 1, 20, 20, 2, 1, 64, 64, torch.float16)
+    q.requires_grad_(True)
+    plain, = torch.autograd.grad(at.attention(q, k, v), q, g)
+    dq, = torch.autograd.grad(at.attention(q, k, v), q, g, create_graph=True)
+    assert torch.equal(plain, dq)
+    with pytest.raises(RuntimeError, match="once_differentiable|does not require grad"):
+        torch.autograd.grad(dq.float().square().sum(), q)
+
+
 def test_gradients_against_differences(at):
     """Directional differences of L = <dout, out>, in 64 bits around the 16-bit point, and the gradients'
     inner products with the direction: to 2 % of the sum of |terms|' root (rounding to 16 bits)."""
