@@ -37,7 +37,8 @@
  *     multiple of 8 (4) elements wide are moved in wide accesses; any other
  *     alignment to the element size is accepted and slower.
  *   - The address range of an output must not overlap that of an input, the
- *     workspace or another output.
+ *     workspace or another output.  (The pages of keys and of values may
+ *     interleave in one allocation.)
  *   - lse is fp32: B x Hq x M (dense) or Hq x M (packed), contiguous.
  *   - Rows of outputs that belong to no sequence are left as they were, or, as
  *     `zero_rest` asks, written as 0 (out and gradients) and -inf (lse).
@@ -89,7 +90,7 @@ typedef struct {
  * the keys at k.data + x * k.batch_stride.  lens: keys of each sequence, those of
  * the call's own tokens included.  A key on a page whose number is outside
  * [0, pages) reads as NaN and is not written; positions from table_width *
- * page_size on do not exist. */
+ * page_size on do not exist, nor does any in a cache of 0 pages. */
 typedef struct {
   gs_attention_array k, v;
   int64_t pages, page_size, table_width;
@@ -99,7 +100,7 @@ typedef struct {
 
 /* out and (unless NULL) lse of every row.  low (unless NULL): what the rounding
  * of out leaves, out - rounded, itself rounded to the dtype, for the backward
- * pass.  M == 0 or B == 0 is a no-op.
+ * pass.  M == 0, or B == 0 in the dense layout, is a no-op.
  * Workspace: gs_attention_fwd_workspace_size(p) bytes (which may be 0). */
 gs_status gs_attention_fwd(const gs_attention_problem* p, const gs_attention_array* q,
                            const gs_attention_array* k, const gs_attention_array* v,

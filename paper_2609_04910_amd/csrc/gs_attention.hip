@@ -131,7 +131,7 @@ namespace {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
 constexpr int64_t kMaxStride = (int64_t)1 << 44;
-constexpr int64_t kMaxGrid = 0x7fffffff;
+constexpr int64_t kMaxGrid = (1ll << 24) - 1;  // workgroups of 256 threads: below 2^32 threads
 
 int padded_width(int64_t D, int64_t C) {
   const int64_t w = D > C ? D : C;
@@ -366,7 +366,7 @@ hipError_t by_type(const gs_attention_problem& p, F f) {
 }
 
 gs_status index_args(const gs_attention_problem& p, const int32_t* q_index, const int32_t* k_index) {
-  if (p.packed && p.B > 0 && (!q_index || !k_index)) return GS_ERR_NULL_POINTER;
+  if (p.packed && (!q_index || !k_index)) return GS_ERR_NULL_POINTER;
   if ((reinterpret_cast<uintptr_t>(q_index) | reinterpret_cast<uintptr_t>(k_index)) & 3) return GS_ERR_MISALIGNED;
   return GS_SUCCESS;
 }
@@ -377,7 +377,7 @@ gs_status run_fwd(const gs_attention_problem* p, const gs_attention_array* q, co
                   hipStream_t stream) {
   gs_status st = check(p);
   if (st != GS_SUCCESS) return st;
-  if (p->B == 0 || p->M == 0) return GS_SUCCESS;
+  if ((p->B == 0 && !p->packed) || p->M == 0) return GS_SUCCESS;
   if ((st = index_args(*p, q_index, k_index)) != GS_SUCCESS) return st;
   const int64_t B = p->packed ? 1 : p->B;
   const FwdPlan f = fwd_plan(*p, false, dense_keys(*p), ws);
@@ -417,7 +417,7 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
   gs_status st = check(p);
   if (st != GS_SUCCESS) return st;
   if (!dq && !dk && !dv) return GS_ERR_NULL_POINTER;
-  if (p->B == 0 || (p->M == 0 && p->N == 0)) return GS_SUCCESS;
+  if ((p->B == 0 && !p->packed) || (p->M == 0 && p->N == 0)) return GS_SUCCESS;
   if ((st = index_args(*p, q_index, k_index)) != GS_SUCCESS) return st;
   const int64_t B = p->packed ? 1 : p->B;
   const BwdPlan w = bwd_plan(*p, dk || dv, ws);
@@ -576,7 +576,8 @@ gs_status run_append(const gs_attention_problem* p, const gs_attention_array* k,
   in[2] = index_span(*p, q_index);
   in[3] = span_of(cache->lens, 4 * p->B);
   in[4] = span_of(cache->table, 4 * p->B * cache->table_width);
-  if (overlaps(o, 2, in, 5)) return GS_ERR_ALIAS;
+  // keys and values may be interleaved in one allocation, but not the same
+  if (overlaps(o, 1, in, 5) || overlaps(o + 1, 1, in, 5) || (cache->pages > 0 && a.kp.p == a.vp.p)) return GS_ERR_ALIAS;
   if (cache->table_width == 0 || cache->pages == 0) return GS_SUCCESS;
   a.s = shape_of(*p, q_index, nullptr);
   a.chunks = (int32_t)(((p->D > p->C ? p->D : p->C) + 7) / 8);
@@ -593,7 +594,7 @@ gs_status run_append(const gs_attention_problem* p, const gs_attention_array* k,
 extern "C" {
 
 size_t gs_attention_fwd_workspace_size(const gs_attention_problem* p) {
-  if (gs::check(p) != GS_SUCCESS || p->B == 0 || p->M == 0) return 0;
+  if (gs::check(p) != GS_SUCCESS || (p->B == 0 && !p->packed) || p->M == 0) return 0;
   return gs::fwd_plan(*p, false, gs::dense_keys(*p), nullptr).total;
 }
 

@@ -163,6 +163,7 @@ def test_paged_refusals():
     assert append(c=cache(k=array(10, 16, 2, 64, head=0))) == 9
     assert append(problem(M=0), cache()) == 0 and append(problem(B=0), cache()) == 0
     assert append(c=cache(width=0, table=None)) == 0 and append(c=cache(pages=0)) == 0
+    assert append(c=cache(v=array(10, 16, 2, 32))) == 9       # keys and values in one place
 
 
 H, BF = torch.float16, torch.bfloat16

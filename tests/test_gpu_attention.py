@@ -271,6 +271,10 @@ def test_strides(at):
     _, dk, dv = at.attention_bwd(q, one[0], one[1], out, lse, g, low=low)   # the same call as autograd's
     torch.testing.assert_close(gk.float(), dk.float().sum(0, keepdim=True), rtol=2 ** -7, atol=1e-4)
     torch.testing.assert_close(gv.float(), dv.float().sum(0, keepdim=True), rtol=2 ** -7, atol=1e-4)
+    buf = torch.full((B * M * H * (D + 1) + 1,), 7.0, dtype=torch.bfloat16, device="cuda")
+    odd_out = buf[1:].view(B, M, H, D + 1)[..., :D]
+    at.attention_fwd(q, k, v, out=odd_out)
+    assert torch.equal(odd_out, at.attention_fwd(q, k, v)[0]) and (buf[1:].view(B, M, H, D + 1)[..., D] == 7).all() and buf[0] == 7
     wide = torch.zeros(B, M, 2 * H, D, dtype=torch.bfloat16, device="cuda")
     at.attention_fwd(q, k, v, out=wide[:, :, ::2])
     assert torch.equal(wide[:, :, ::2], at.attention_fwd(q, k, v)[0]) and not wide[:, :, 1::2].any()
@@ -429,6 +433,69 @@ def test_no_rows_or_no_keys(at):
         assert not out.any() and (lse == -math.inf).all()
         for t, like in ((dq, q), (dk, k), (dv, v)):
             assert t.shape == like.shape and not t.any()
+
+
+def test_packed_without_sequences(at):
+    """One offset, no sequence: every row is one of none."""
+    gen = torch.Generator().manual_seed(26)
+    q, k, v = (normal(gen, (n, 2, 64), torch.float16) for n in (40, 3000, 3000))
+    offs = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = at.attention_fwd(q, k, v, q_offsets=offs)
+    assert not out.any() and (lse == -math.inf).all()
+    for t in at.attention_bwd(q, k, v, out, lse, torch.ones_like(out), q_offsets=offs):
+        assert not t.any()
+
+
+def test_captured_autograd_step_replays(at):
+    """The step through autograd, captured with leaves of its own (a leaf that an eager graph holds would
+    bring that graph's stream into the capture)."""
+    q, k, v, g = make(27, 2, 70, 70, 4, 2, 64, 64, torch.bfloat16)
+
+    def step(leaves):
+        out = at.attention(*leaves, causal=True)
+        return (out.detach(),) + torch.autograd.grad(out, leaves, g)
+
+    eager = [t.clone() for t in step([t.clone().requires_grad_(True) for t in (q, k, v)])]
+    mine = [t.clone().requires_grad_(True) for t in (q, k, v)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(mine)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step(mine)
+    for _ in range(3):
+        for t in held:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, eager):
+            assert torch.equal(a, b)
+
+
+def test_threads(at):
+    """Calls from several host threads at once, each on a stream of its own."""
+    import threading
+    sets = [make(30 + i, 1, 100 + i, 150, 2, 1, 64, 64, torch.float16) for i in range(4)]
+    want = [at.attention_fwd(q, k, v)[0] for q, k, v, _ in sets]
+    torch.cuda.synchronize()
+    got, streams = [None] * 4, [torch.cuda.Stream() for _ in range(4)]
+
+    def work(i):
+        q, k, v, _ = sets[i]
+        for _ in range(50):
+            got[i] = at.attention_fwd(q, k, v, stream=streams[i])[0]
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
 
 
 def test_captured_step_replays(at):

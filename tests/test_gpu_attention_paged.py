@@ -128,6 +128,49 @@ def test_bad_page_numbers(at, rows, number):
     assert set(changed) == {cache.pages[0][5], cache.pages[0][6], cache.pages[1][6]}
 
 
+def test_interleaved_and_strided_pages(at):
+    """Keys and values as views of one allocation, heads before rows in a page."""
+    gen = torch.Generator().manual_seed(7)
+    both = torch.full((9, 2, 2, 16, 64), math.nan, dtype=torch.bfloat16, device="cuda")   # page, k/v, head, row, column
+    kp, vp = both[:, 0].transpose(1, 2), both[:, 1].transpose(1, 2)
+    table = torch.tensor([[4, 1, 7], [8, 0, 3]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([40, 33], dtype=torch.int32, device="cuda")
+    k, v = normal(gen, (73, 2, 64), torch.bfloat16), normal(gen, (73, 2, 64), torch.bfloat16)
+    at.attention_append(k, v, kp, vp, table, lens, q_offsets=offsets([40, 33]))
+    for rows in ([1, 1], [5, 33]):
+        q = normal(gen, (sum(rows), 4, 64), torch.bfloat16)
+        out = at.attention_paged(q, kp, vp, table, lens, q_offsets=offsets(rows))
+        for b, part in enumerate((slice(0, 40), slice(40, 73))):
+            i = slice(sum(rows[:b]), sum(rows[:b + 1]))
+            ref.check("out", out[i], *ref.one(q[i], k[part], v[part], 0.125, True)["out"])
+
+
+def test_no_pages_and_no_sequences(at):
+    q = torch.ones((2, 2, 64), dtype=torch.float16, device="cuda")
+    empty = torch.empty((0, 16, 1, 64), dtype=torch.float16, device="cuda")
+    table, lens = torch.zeros((2, 3), dtype=torch.int32, device="cuda"), torch.full((2,), 20, dtype=torch.int32, device="cuda")
+    out, lse = at.attention_paged(q, empty, empty.clone(), table, lens, return_lse=True)
+    assert not out.any() and (lse == -math.inf).all()
+    at.attention_append(q[:, :1], q[:, :1], empty, empty.clone(), table, lens)
+    pages = torch.ones((4, 16, 1, 64), dtype=torch.float16, device="cuda")
+    offs = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = at.attention_paged(q, pages, pages.clone(), table[:0], lens[:0], q_offsets=offs, return_lse=True)
+    assert not out.any() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_long_cache(at, rows):
+    """70001 keys, scores spread so that early keys weigh as late ones do."""
+    gen = torch.Generator().manual_seed(8)
+    cache = Cache(gen, [70001, 5], 64, 1, 64, 64, torch.bfloat16)
+    q = normal(gen, (rows + 5, 2, 64), torch.bfloat16, std=0.5)
+    out, lse = at.attention_paged(q, cache.k, cache.v, cache.table, cache.lens, q_offsets=offsets([rows, 5]), return_lse=True)
+    for b, i in enumerate((slice(0, rows), slice(rows, rows + 5))):
+        r = ref.one(q[i], *cache.keys[b], 0.125, True)
+        ref.check("out", out[i], *r["out"])
+        ref.check("lse", lse[:, i], *r["lse"])
+
+
 def test_lengths_past_the_table(at):
     """More keys than the table holds: the sequence ends with the table."""
     gen = torch.Generator().manual_seed(3)
