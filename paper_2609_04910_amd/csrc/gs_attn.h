@@ -135,15 +135,19 @@ __device__ __forceinline__ int packed_tile(const int32_t* off, int B, int rows, 
 // (sequence, head) streams every XCD gets a contiguous run of them, so the query
 // heads that share a key head read its keys through one L2.
 //
-// The caller counts tiles from the one with most pairs (causal masks).  The first
-// 256 blocks go to a CU each and the next 256 join them: those are turned round, so
-// that the CU of the longest block gets the shortest of them.
-__device__ __forceinline__ void block_place(int id, int heads, int tiles, int& tile, int& head) {
+// The caller counts tiles from the one with most pairs.
+__device__ __forceinline__ void block_place(int id, int heads, int& tile, int& head) {
   tile = id / heads;
   const int p = id - tile * heads;
   head = (heads & 7) == 0 ? (p & 7) * (heads >> 3) + (p >> 3) : p;
-  const int row = 256 / heads;
-  if (tile >= row && tile < 2 * row) tile = row + min(2 * row, tiles) - 1 - tile;
+}
+
+// Where two workgroups share a CU the first 256 blocks go to a CU each and the next
+// 256 join them: those are turned round, eight by eight (so that each stays on its
+// XCD), and the CU of the longest block gets the shortest of them.
+__device__ __forceinline__ int folded(int id, int blocks) {
+  const int groups = (min(blocks, 512) - 256) >> 3, g = (id - 256) >> 3;
+  return id < 256 || g >= groups ? id : 256 + ((groups - 1 - g) << 3) + (id & 7);
 }
 
 // Rows that column point `at` (its index in its sequence) sees on the other

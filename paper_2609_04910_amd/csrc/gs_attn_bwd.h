@@ -199,8 +199,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
   const int col = lane & 15, g = lane >> 4;
 
   int tile, head, b;
-  const int split = KV ? blockIdx.x / a.wgs : 0;
-  block_place(blockIdx.x - split * a.wgs, a.heads, a.tiles, tile, head);
+  const int id = folded(blockIdx.x, gridDim.x), split = KV ? id / a.wgs : 0;
+  block_place(id - split * a.wgs, a.heads, tile, head);
   const int rows_all = KV ? s.N : s.M;
   if (s.packed) {
     const int slot = tile;

@@ -239,11 +239,12 @@ __device__ __forceinline__ int by_length(const int32_t* lens, int B, int rank) {
 }
 
 // Returns whether there is anything to do (rows of no sequence are handled here).
-// SORT: where no two workgroups share keys, the sequences of most keys first.
-template <int ROWS, bool PAGED, bool SORT>
+// FOLD: two workgroups share a CU.  Not so for few rows, where no two workgroups
+// share keys either: there (paged) the sequences of most keys come first.
+template <int ROWS, bool PAGED, bool FOLD>
 __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
   const AttnShape& s = a.s;
-  int id = blockIdx.x;
+  int id = FOLD ? folded(blockIdx.x, gridDim.x) : blockIdx.x;
   w.part = 0;
   if (a.splits > 1) {
     // all first parts, then all second ones, ...: parts without keys then fall on
@@ -252,7 +253,7 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
     id -= w.part * a.wgs;
   }
   int tile, head;
-  block_place(id, a.heads, a.tiles, tile, head);
+  block_place(id, a.heads, tile, head);
   if (s.packed) {
     const int slot = tile;
     int n;
@@ -276,7 +277,7 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
     tile = n - 1 - tile;  // the tiles that see most keys first
   } else {
     const int per_seq = a.heads / s.B;
-    if (SORT) {
+    if (PAGED && !FOLD) {
       const int p = id % a.heads;
       w.b = by_length(a.pg.lens, s.B, p / per_seq);
       head = p % per_seq;
@@ -498,7 +499,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 
   AttnJob job;
-  if (!attn_job<ROWS, PAGED, false>(a, job)) return;
+  if (!attn_job<ROWS, PAGED, true>(a, job)) return;
   const int kn = job.sq.kn, wr0 = job.r0 + wave * 16 * NQ;
   AttnRows<T, DP, NQ> rows;
   rows.start(a, job, wr0);
@@ -604,7 +605,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 
   AttnJob job;
-  if (!attn_job<ROWS, PAGED, PAGED>(a, job)) return;
+  if (!attn_job<ROWS, PAGED, false>(a, job)) return;
   const int kn = job.sq.kn;
   AttnRows<T, DP, NQ> rows;
   rows.start(a, job, job.r0);
