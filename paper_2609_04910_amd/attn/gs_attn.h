@@ -20,7 +20,7 @@
 // chunk c ^ swz(row), so that the operand reads spread over the LDS banks.
 #pragma once
 
-#include "gs_common.h"
+#include "../csrc/gs_common.h"
 
 namespace gs {
 

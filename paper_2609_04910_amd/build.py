@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "gauss_sum.hip")
 LIB = os.path.join(HERE, "libgauss_sum.so")
-ATTENTION_SRC = os.path.join(HERE, "csrc", "gs_attention.hip")
+ATTENTION_SRC = os.path.join(HERE, "attn", "gs_attention.hip")
 ATTENTION_LIB = os.path.join(HERE, "libgs_attention.so")
 PEAKS_SRC = os.path.join(HERE, "peaks", "gs_peaks.hip")
 PEAKS_LIB = os.path.join(HERE, "libgs_peaks.so")
@@ -34,7 +34,7 @@ FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
-    """Compile csrc/gauss_sum.hip into libgauss_sum.so, csrc/gs_attention.hip
+    """Compile csrc/gauss_sum.hip into libgauss_sum.so, attn/gs_attention.hip
     into libgs_attention.so and peaks/gs_peaks.hip into libgs_peaks.so; returns
     the path of libgauss_sum.so."""
     compile_one(PEAKS_SRC, PEAKS_LIB, verbose)
@@ -81,8 +81,8 @@ def compile_one(src: str, lib: str, verbose: bool) -> str:
 
 
 def sources():
-    d = os.path.join(HERE, "csrc")
-    return [os.path.join(d, f) for f in sorted(os.listdir(d))] + [
+    dirs = [os.path.join(HERE, "csrc"), os.path.join(HERE, "attn")]
+    return [os.path.join(d, f) for d in dirs for f in sorted(os.listdir(d))] + [
         os.path.join(ROOT, "include", "gauss_sum.h"), os.path.join(ROOT, "include", "gs_attention.h")]
 
 
