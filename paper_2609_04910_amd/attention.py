@@ -37,6 +37,7 @@ LIB_PATH = os.path.join(HERE, "libgs_attention.so")
 EXPORTED = ("gs_attention_fwd", "gs_attention_fwd_workspace_size", "gs_attention_bwd",
             "gs_attention_bwd_workspace_size", "gs_attention_paged", "gs_attention_paged_workspace_size",
             "gs_attention_append")
+MAX_DIM = 256  # GAUSS_SUM_MAX_DIM
 REST_OUT, REST_LSE = 1, 2  # GS_ATTENTION_REST_OUT, GS_ATTENTION_REST_LSE
 
 
@@ -124,6 +125,11 @@ def _check_columns(name, t, dims):
         raise ValueError("the columns of %s must be contiguous" % name)
 
 
+def _check_widths(D, C):
+    if not (1 <= D <= MAX_DIM and 1 <= C <= MAX_DIM):
+        raise ValueError("D and C must be 1 to %d, got %d and %d" % (MAX_DIM, D, C))
+
+
 def _check_index(name, t, n, device):
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != torch.int32:
@@ -174,6 +180,7 @@ def _check_call(q, k, v, causal, window, q_offsets, k_offsets, q_lens, k_lens):
         raise ValueError("%d query heads over %d key heads: must be a multiple" % (Hq, Hkv))
     if not packed and q.shape[0] != k.shape[0]:
         raise ValueError("q has %d sequences, k has %d" % (q.shape[0], k.shape[0]))
+    _check_widths(D, v.shape[-1])
     if window < 0 or (window and not causal):
         raise ValueError("window must be 0, or positive with causal")
     _dtype(("q", q), ("k", k), ("v", v))
@@ -200,7 +207,7 @@ class _Call:
         # the usual call, told by its sizes alone; any other goes through the checks
         if not (q_offsets is None and q_lens is None and k_lens is None and k_offsets is None
                 and len(qs) == 4 and len(vs) == 4 and window == 0 and ks == (qs[0], vs[1], vs[2], qs[3])
-                and vs[2] and qs[2] and qs[2] % vs[2] == 0 and vs[0] == qs[0]
+                and 0 < qs[3] <= MAX_DIM and 0 < vs[3] <= MAX_DIM and vs[2] and qs[2] and qs[2] % vs[2] == 0 and vs[0] == qs[0]
                 and q.dtype in _dtypes() and k.dtype == q.dtype and v.dtype == q.dtype
                 and q.stride(3) == 1 and k.stride(3) == 1 and v.stride(3) == 1
                 and self.gpu >= 0 and k.get_device() == self.gpu and v.get_device() == self.gpu):
@@ -425,6 +432,7 @@ def _cache_call(x, name, k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, 
     if k_pages.shape[:3] != v_pages.shape[:3] or k_pages.shape[3] != D or v_pages.shape[3] != C:
         raise ValueError("k_pages must be pages x page_size x Hkv x %d and v_pages the same x %d, got %s and %s"
                          % (D, C, tuple(k_pages.shape), tuple(v_pages.shape)))
+    _check_widths(D, C)
     if k_pages.shape[1] < 1:
         raise ValueError("pages must hold at least one row")
     if Hkv < 1 or Hq % Hkv or Hq == 0:

@@ -229,13 +229,8 @@ __device__ __forceinline__ void copy4(const void* base, uint32_t off, uint32_t l
                : "memory", "m0");
 }
 
-// At most LEFT copies of this wave still in flight (they complete in order), and
-// no LDS access of it.
-template <int LEFT>
-__device__ __forceinline__ void copies_left() {
-  static_assert(LEFT < 64, "vmcnt range");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(LEFT) : "memory");
-}
+// Every copy of this wave has landed, and no LDS access of it is under way.
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // The workgroup's barrier, with this wave's LDS writes done.
 __device__ __forceinline__ void tile_barrier() {
@@ -467,11 +462,17 @@ __device__ __forceinline__ float left(float x) {
   return x - T::to_float((uint16_t)pack2<T>(x, 0.0f));
 }
 
-// Zeros in rows first + part, first + part + parts, ... < rows of one head.
-__device__ __forceinline__ void zero_rows(const AttnArray& x, int b, int head, int width, int first, int rows,
-                                          int part, int parts) {
-  for (int64_t r = first + part; r < rows; r += parts) {
-    uint16_t* p = reinterpret_cast<uint16_t*>(x.p + b * x.sb + r * x.sr + head * x.sh);
+// Whether row i of packed rows belongs to a sequence (the offsets not decreasing).
+__device__ __forceinline__ bool in_sequences(const int32_t* off, int B, int i) {
+  return B > 0 && i >= off[0] && i < off[B];
+}
+
+// Zeros in the rows of no sequence among rows part, part + parts, ... of one head.
+__device__ __forceinline__ void zero_rest_rows(const AttnArray& x, int head, int width, const int32_t* off, int B,
+                                               int rows, int part, int parts) {
+  for (int64_t r = part; r < rows; r += parts) {
+    if (in_sequences(off, B, (int)r)) continue;
+    uint16_t* p = reinterpret_cast<uint16_t*>(x.p + r * x.sr + head * x.sh);
     for (int c = threadIdx.x; c < width; c += blockDim.x) p[c] = 0;
   }
 }

@@ -7,8 +7,12 @@
 //
 // k_attn_fwd: a workgroup of NW waves streams 64-key (DP = 256: 32-key) tiles of K
 // and V through an LDS ring, one barrier a tile; wave w owns 16*NQ rows whose query
-// operands and output sums stay in registers.  Bound by the matrix cores.
-// k_attn_rows: the same for few rows, bound by reading K and V.
+// operands and output sums stay in registers.  Bound by the matrix cores: 16384
+// tokens, 16 query and 4 key heads, D = 128, causal 982 us, 1.12 PFLOP/s (a library
+// product of 8192 cubed: 1.28).
+// k_attn_rows: the same for few rows, bound by reading K and V: one token of 64
+// sequences of 4096 keys, 8 key heads, D = 128 208 us, 5.2 TB/s (a streaming read:
+// 5.6).
 // Both can work on a part of a row's keys; k_attn_join then joins the parts.
 #pragma once
 
@@ -86,13 +90,10 @@ struct PageSlice {
   __device__ __forceinline__ int number(const AttnPages& pg, int j) const { return e[page_index(pg, j) - first]; }
 };
 
+// Keys (rows) of a streamed tile: two stages of K and V take 64 KiB, so two
+// workgroups share a CU.  (32-key tiles in three or four stages: 4 - 10 % slower.)
 template <int DP>
 constexpr int attn_keys() { return DP == 256 ? 32 : 64; }
-
-template <int DP, bool PAGED>
-constexpr int attn_stages() { return 2; }
-template <int DP, bool PAGED>
-constexpr int attn_tile() { return attn_keys<DP>(); }
 
 // Query operand: columns 32c + 8g .. +7 of one row, zero past the width.
 template <typename T>
@@ -148,9 +149,8 @@ __device__ __forceinline__ void copy_pages(const AttnFwdArgs& a, const PageSlice
 
 // Sets the bits of the lane's results that infinities among the values of a tile
 // reach: +inf in the first NB words of each column tile, -inf in the next, NaN in
-// both (inf - inf is NaN).  The values are
-// read from the caller's array again; products of indicators tell which columns
-// see a row that has one.
+// both (inf - inf is NaN).  The values are read from the caller's array again;
+// products of indicators tell which columns see a row that has one.
 template <typename T, int DP, int BK, int NQ, bool PAGED, int NB2>
 __device__ __forceinline__ void found_infinities(const AttnFwdArgs& a, const char* vb, int b, int kn, int key0,
                                               const int (&lo)[NQ], const int (&hi)[NQ], uint32_t (&bits)[NB2],
@@ -261,15 +261,14 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
     if (w.b == kNoRow) {  // slots past the last tile: rows of no sequence
       if (s.zero_rest && w.part == 0) {
         const int part = slot - tile, parts = a.tiles - tile;
-        const int end = s.B > 0 ? clampi(s.q_index[s.B], 0, s.M) : 0;
         for (int h = head * a.per; h < (head + 1) * a.per; ++h) {
           if (s.zero_rest & kRestOut) {
-            zero_rows(a.out, 0, h, s.C, end, s.M, part, parts);
-            if (a.low.p) zero_rows(a.low, 0, h, s.C, end, s.M, part, parts);
+            zero_rest_rows(a.out, h, s.C, s.q_index, s.B, s.M, part, parts);
+            if (a.low.p) zero_rest_rows(a.low, h, s.C, s.q_index, s.B, s.M, part, parts);
           }
           if (a.lse && (s.zero_rest & kRestLse))
-            for (int64_t r = end + part; r < s.M; r += parts)
-              if (threadIdx.x == 0) a.lse[h * a.lse_sh + r] = -__builtin_inff();
+            for (int64_t r = part; r < s.M; r += parts)
+              if (threadIdx.x == 0 && !in_sequences(s.q_index, s.B, (int)r)) a.lse[h * a.lse_sh + r] = -__builtin_inff();
         }
       }
       return false;
@@ -488,9 +487,9 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
 
 template <typename T, int DP, int NQ, int NW, bool PAGED, bool WIDE>
 __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
-  constexpr int BK = attn_tile<DP, PAGED>(), NS = attn_stages<DP, PAGED>(), NO = DP / 16, TILE = BK * DP * 2, ROWS = 16 * NQ * NW;
+  constexpr int BK = attn_keys<DP>(), NO = DP / 16, TILE = BK * DP * 2, ROWS = 16 * NQ * NW;
   constexpr int NB = (NO * 4 + 31) / 32;
-  __shared__ __align__(1024) char smem[NS * 2 * TILE];
+  __shared__ __align__(1024) char smem[2 * 2 * TILE];
   __shared__ int mark[4];
   // infinities that reach the lane's results: bit 4 ct + r of its column tile n
   __shared__ uint32_t inf_bits[64 * NW][2 * NQ * NB];
@@ -530,7 +529,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
   };
 
   if (s.D < DP || s.C < DP) {
-    clear_tiles<64 * NW>(smem, NS * 2 * TILE);
+    clear_tiles<64 * NW>(smem, 2 * 2 * TILE);
     __syncthreads();
   }
   bool infinities = false;
@@ -544,21 +543,15 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
       pages.load(a.pg, slice, job.b, from, to, 64 * NW);
       rows.max_key = to - 1;
     }
-#pragma unroll
-    for (int k = 0; k < NS - 1; ++k)
-      if (from + k * BK < to) issue(from + k * BK, k, to);
+    issue(from, 0, to);
     int stage = 0;
-    for (int key0 = from; key0 < to; key0 += BK) {
+    for (int key0 = from; key0 < to; key0 += BK, stage ^= 1) {
       ++it;
-      // this tile's copies are done; those of the NS - 2 next ones may be in flight
-      if (key0 + (NS - 2) * BK < to)
-        copies_left<(NS - 2) * 2 * TileCopy<DP, BK, 64 * NW>::N>();
-      else
-        copies_left<0>();
+      copies_done();
       const bool bordered = key0 + BK > all.in_hi || key0 < all.in_lo;
       if (bordered && clean_tile<T, DP, BK, 64 * NW>(smem + (stage * 2 + 1) * TILE, threadIdx.x)) mark[it & 3] = it;
-      tile_barrier();  // this tile has landed everywhere, and nobody reads the stage before it
-      if (key0 + (NS - 1) * BK < to) issue(key0 + (NS - 1) * BK, stage == 0 ? NS - 1 : stage - 1, to);
+      tile_barrier();  // this tile has landed everywhere, and nobody reads the other stage
+      if (key0 + BK < to) issue(key0 + BK, stage ^ 1, to);
       if (bordered && uniform(mark[it & 3]) == it) {
         found_infinities<T, DP, BK, NQ, PAGED>(a, vb, job.b, kn, key0, rows.lo, rows.hi, inf_bits[threadIdx.x],
                                                !infinities);
@@ -569,7 +562,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
         const bool masked = key0 + BK > mine.in_hi || key0 < mine.in_lo;
         rows.template attend<BK / 32>(a, kt, kt + TILE, ln, key0, masked, PAGED ? &pages : nullptr);
       }
-      stage = stage + 1 == NS ? 0 : stage + 1;
     }
     from = to;
   }
@@ -650,7 +642,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
     if (from + 32 * wave < to) issue(from + 32 * wave, 0, to);
     int stage = 0;
     for (int key0 = from + 32 * wave; key0 < to; key0 += step, stage ^= 1) {
-      copies_left<0>();  // this tile has landed, and nothing reads the other stage
+      copies_done();  // this tile has landed, and nothing reads the other stage
       if (key0 + step < to) issue(key0 + step, stage ^ 1, to);
       char* kt = ring + stage * 2 * TILE;
       const bool masked = key0 + 32 > all.in_hi || key0 < all.in_lo;
@@ -722,8 +714,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
   char* low = a.low.p ? a.low.p + b * a.low.sb + row * a.low.sr + h * a.low.sh : nullptr;
   float* lse = a.lse ? a.lse + b * a.lse_sb + h * a.lse_sh + row : nullptr;
   if (s.packed) {
-    // rows of no sequence are written, or left, by the main kernel
-    if (row < clampi(s.q_index[0], 0, s.M) || row >= clampi(s.q_index[s.B], 0, s.M)) return;
+    if (!in_sequences(s.q_index, s.B, (int)row)) return;  // written, or left, by the main kernel
   } else if (s.q_index && row >= clampi(s.q_index[b], 0, s.M)) {
     if (s.zero_rest & kRestOut)
       for (int c = lane; c < s.C; c += 64) {

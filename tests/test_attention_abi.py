@@ -187,6 +187,8 @@ def i32(*x):
     ((z(1, 5, 2, 8), z(1, 6, 2, 8, dtype=BF), z(1, 6, 2, 4)), {}, TypeError, "share a dtype"),
     ((z(1, 5, 2, 8, dtype=torch.float32), z(1, 6, 2, 8), z(1, 6, 2, 4)), {}, TypeError, "float16 or bfloat16"),
     ((z(1, 8, 2, 5).transpose(1, 3), z(1, 6, 2, 8), z(1, 6, 2, 4)), {}, ValueError, "contiguous"),
+    ((z(1, 5, 2, 0), z(1, 6, 2, 0), z(1, 6, 2, 4)), {}, ValueError, "D and C"),
+    ((z(1, 5, 2, 8), z(1, 6, 2, 8), z(1, 6, 2, 257)), {}, ValueError, "D and C"),
     ((z(1, 5, 2, 8), z(1, 6, 2, 8), z(1, 6, 2, 4)), dict(window=3), ValueError, "window"),
     ((z(1, 5, 2, 8), z(1, 6, 2, 8), z(1, 6, 2, 4)), dict(window=-3, causal=True), ValueError, "window"),
     ((z(1, 5, 2, 8), z(1, 6, 2, 8), z(1, 6, 2, 4)), dict(k_lens=torch.tensor([3])), TypeError, "int32"),

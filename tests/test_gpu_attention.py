@@ -435,6 +435,24 @@ def test_no_rows_or_no_keys(at):
             assert t.shape == like.shape and not t.any()
 
 
+def test_packed_rows_before_the_first_sequence(at):
+    """Offsets that do not start at 0: the rows before them belong to no sequence."""
+    gen = torch.Generator().manual_seed(28)
+    q, k, v, g = (normal(gen, (60, 2, 64), torch.bfloat16) for _ in range(4))
+    for t in (q, k, v, g):
+        t[:7] = float("nan")
+    offs = torch.tensor([7, 30, 50], dtype=torch.int32, device="cuda")
+    out, lse = at.attention_fwd(q, k, v, q_offsets=offs, causal=True)
+    grads = at.attention_bwd(q, k, v, out, lse, g, q_offsets=offs, causal=True)
+    for i in (slice(7, 30), slice(30, 50)):
+        r = ref.one(q[i], k[i], v[i], 0.125, True, dout=g[i])
+        for name, t in (("out", out[i]), ("lse", lse[:, i]), ("dq", grads[0][i]), ("dk", grads[1][i]), ("dv", grads[2][i])):
+            ref.check(name, t, *r[name])
+    for t in (out,) + grads:
+        assert not t[:7].any() and not t[50:].any()
+    assert (lse[:, :7] == -math.inf).all() and (lse[:, 50:] == -math.inf).all()
+
+
 def test_packed_without_sequences(at):
     """One offset, no sequence: every row is one of none."""
     gen = torch.Generator().manual_seed(26)
