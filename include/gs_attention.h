@@ -77,7 +77,7 @@ typedef struct {
   int32_t dtype;            /* GS_F16 or GS_BF16 */
   int32_t packed, causal;   /* 0 or 1 */
   int32_t zero_rest;        /* GS_ATTENTION_REST_* flags */
-  float scale;              /* finite */
+  float scale;              /* finite, also times log2 e */
 } gs_attention_problem;
 
 typedef struct {

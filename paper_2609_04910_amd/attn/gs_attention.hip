@@ -146,7 +146,8 @@ gs_status check(const gs_attention_problem* p) {
       p->window > kMaxRows || (p->window > 0 && !p->causal))
     return GS_ERR_BAD_SHAPE;
   if (p->dtype != GS_F16 && p->dtype != GS_BF16) return GS_ERR_UNSUPPORTED;
-  if (!(p->scale > -__builtin_inff()) || !(p->scale < __builtin_inff())) return GS_ERR_BAD_TAU;
+  const float c = p->scale * kLog2e;  // what the kernels use is finite as well
+  if (!(c > -__builtin_inff()) || !(c < __builtin_inff())) return GS_ERR_BAD_TAU;
   return GS_SUCCESS;
 }
 
@@ -258,7 +259,9 @@ FwdPlan fwd_plan(const gs_attention_problem& p, bool paged, int64_t keys, void* 
   f.rows = !few ? attn_fwd_rows(DP) : shared <= 16 ? 16 : rows_most(DP);
   f.tiles = tiles_of(p, p.M * f.per, f.rows);
   f.heads = (f.per > 1 || G == 1 ? p.Hkv : p.Hq) * B;
-  // With fewer workgroups than two a CU a row's keys are cut into parts
+  // With fewer workgroups than two a CU a row's keys are cut into parts, none
+  // shorter than 256 (512) keys.  Chunks of up to 512 tokens over 3000 to 12000 keys:
+  // 256 workgroups 408 us, 512 283 us, 768 307 us, 1024 299 us
   const int64_t wgs = f.tiles * f.heads, want = 512, least = few ? kLeastPart : 512;
   f.splits = wgs > 0 && keys >= 2 * least
                  ? std::max<int64_t>(1, std::min({want / wgs, keys / least, (int64_t)kMostParts}))

@@ -69,7 +69,7 @@ BIG = 1 << 31
     (dict(Hq=0), 2), (dict(Hkv=0), 2), (dict(Hq=1 << 15), 2), (dict(D=0), 2), (dict(D=257), 2), (dict(C=0), 2),
     (dict(C=257), 2), (dict(window=-1), 2), (dict(window=3), 2), (dict(window=BIG, causal=1), 2),
     (dict(dtype=gs.GS_F32), 4), (dict(dtype=9), 4), (dict(scale=float("nan")), 3), (dict(scale=float("inf")), 3),
-    (dict(B=0), 0), (dict(M=0), 0),
+    (dict(scale=3e38), 3), (dict(scale=-3e38), 3), (dict(B=0), 0), (dict(M=0), 0),
     (dict(packed=1), 1),                                      # no offsets
     (dict(B=1 << 20, M=1 << 30, Hq=1, Hkv=1), 2),             # more tiles than a grid holds
 ])
