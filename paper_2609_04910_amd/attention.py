@@ -527,10 +527,13 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
         lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
         rest |= REST_LSE
     if sizes[0] == 0:  # no sequences: every row is one of none
-        if rest & REST_OUT:
-            out.zero_()
-        if lse is not None:
-            lse.fill_(float("-inf"))
+        with torch.cuda.stream(stream):
+            if rest & REST_OUT:
+                out.zero_()
+            if lse is not None:
+                lse.fill_(float("-inf"))
+        if stream is not None:
+            gs._keep_alive(stream, out, lse)
         return (out, lse) if return_lse else out
     need = _paged_bytes(sizes, modes, k_pages.shape[1], page_table.shape[1])
     wbytes = 0

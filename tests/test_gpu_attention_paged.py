@@ -158,6 +158,24 @@ def test_no_pages_and_no_sequences(at):
     assert not out.any() and (lse == -math.inf).all()
 
 
+def test_no_sequences_on_another_stream(at):
+    """The rows are written on the given stream, not behind the current one's work."""
+    q = torch.ones((2, 2, 64), dtype=torch.float16, device="cuda")
+    pages = torch.ones((4, 16, 1, 64), dtype=torch.float16, device="cuda")
+    table, none = torch.zeros((0, 3), dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    offs, side = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.cuda.Stream()
+    at.attention_paged(q, pages, pages, table, none, q_offsets=offs, return_lse=True, stream=side)
+    dirty = [torch.full((2, 2, 64), math.nan, dtype=torch.float16, device="cuda"), torch.full((2, 2), math.nan, device="cuda")]
+    torch.cuda.synchronize()
+    del dirty
+    torch.cuda._sleep(200_000_000)
+    out, lse = at.attention_paged(q, pages, pages, table, none, q_offsets=offs, return_lse=True, stream=side)
+    with torch.cuda.stream(side):
+        out, lse = out.cpu(), lse.cpu()
+    torch.cuda.synchronize()
+    assert not out.any() and (lse == -math.inf).all()
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_a_long_cache(at, rows):
     """70001 keys, scores spread so that early keys weigh as late ones do."""
