@@ -335,7 +335,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       const bool bordered = row0 + BR > all_hi || row0 < all_lo;
       if (bordered) {
         char* t = smem + stage * 2 * TILE;
-        const bool x_bad = clean_tile<T, DP, BR, 64 * NW>(t, tid), y_bad = clean_tile<T, DP, BR, 64 * NW>(t + TILE, tid);
+        const bool x_bad = clean_tile<T, DP, BR, 64 * NW>(t, tid);
+        const bool y_bad = clean_tile<T, DP, BR, 64 * NW>(t + TILE, tid);
         if (x_bad || y_bad) mark[it & 3] = it;
       }
       tile_barrier();
