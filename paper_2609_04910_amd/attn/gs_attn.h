@@ -467,12 +467,22 @@ __device__ __forceinline__ bool in_sequences(const int32_t* off, int B, int i) {
   return B > 0 && i >= off[0] && i < off[B];
 }
 
-// Zeros in the rows of no sequence among rows part, part + parts, ... of one head.
-__device__ __forceinline__ void zero_rest_rows(const AttnArray& x, int head, int width, const int32_t* off, int B,
-                                               int rows, int part, int parts) {
-  for (int64_t r = part; r < rows; r += parts) {
-    if (in_sequences(off, B, (int)r)) continue;
-    uint16_t* p = reinterpret_cast<uint16_t*>(x.p + r * x.sr + head * x.sh);
+// The rows of no sequence, before the first and behind the last, in turn.
+struct RestRows {
+  int lo, hi, n;
+  __device__ __forceinline__ RestRows(const int32_t* off, int B, int rows) {
+    lo = B > 0 ? clampi(off[0], 0, rows) : 0;
+    hi = B > 0 ? clampi(off[B], lo, rows) : 0;
+    n = lo + rows - hi;
+  }
+  __device__ __forceinline__ int64_t row(int i) const { return i < lo ? i : hi + (i - lo); }
+};
+
+// Zeros in rows part, part + parts, ... of them, of one head.
+__device__ __forceinline__ void zero_rest_rows(const AttnArray& x, int head, int width, const RestRows& rest, int part,
+                                               int parts) {
+  for (int64_t i = part; i < rest.n; i += parts) {
+    uint16_t* p = reinterpret_cast<uint16_t*>(x.p + rest.row((int)i) * x.sr + head * x.sh);
     for (int c = threadIdx.x; c < width; c += blockDim.x) p[c] = 0;
   }
 }

@@ -212,12 +212,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
     if (b == kNoRow) {
       if ((s.zero_rest & kRestOut) && split == 0) {
         const int part = slot - tile, parts = a.tiles - tile;
-        const int32_t* index = KV ? s.k_index : s.q_index;
+        const RestRows rest(KV ? s.k_index : s.q_index, s.B, rows_all);
         if (KV) {
-          if (a.dk.p) zero_rest_rows(a.dk, head, s.D, index, s.B, rows_all, part, parts);
-          if (a.dv.p) zero_rest_rows(a.dv, head, s.C, index, s.B, rows_all, part, parts);
+          if (a.dk.p) zero_rest_rows(a.dk, head, s.D, rest, part, parts);
+          if (a.dv.p) zero_rest_rows(a.dv, head, s.C, rest, part, parts);
         } else {
-          zero_rest_rows(a.dq, head, s.D, index, s.B, rows_all, part, parts);
+          zero_rest_rows(a.dq, head, s.D, rest, part, parts);
         }
       }
       return;

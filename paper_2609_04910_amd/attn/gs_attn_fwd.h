@@ -261,14 +261,15 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
     if (w.b == kNoRow) {  // slots past the last tile: rows of no sequence
       if (s.zero_rest && w.part == 0) {
         const int part = slot - tile, parts = a.tiles - tile;
+        const RestRows rest(s.q_index, s.B, s.M);
         for (int h = head * a.per; h < (head + 1) * a.per; ++h) {
           if (s.zero_rest & kRestOut) {
-            zero_rest_rows(a.out, h, s.C, s.q_index, s.B, s.M, part, parts);
-            if (a.low.p) zero_rest_rows(a.low, h, s.C, s.q_index, s.B, s.M, part, parts);
+            zero_rest_rows(a.out, h, s.C, rest, part, parts);
+            if (a.low.p) zero_rest_rows(a.low, h, s.C, rest, part, parts);
           }
           if (a.lse && (s.zero_rest & kRestLse))
-            for (int64_t r = part; r < s.M; r += parts)
-              if (threadIdx.x == 0 && !in_sequences(s.q_index, s.B, (int)r)) a.lse[h * a.lse_sh + r] = -__builtin_inff();
+            for (int64_t i = part + (int64_t)threadIdx.x * parts; i < rest.n; i += (int64_t)blockDim.x * parts)
+              a.lse[h * a.lse_sh + rest.row((int)i)] = -__builtin_inff();
         }
       }
       return false;
