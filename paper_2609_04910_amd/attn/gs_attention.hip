@@ -42,6 +42,9 @@ constexpr int rows_waves(int DP) { return DP == 256 ? 2 : 4; }
 constexpr int rows_most(int DP) { return DP == 256 ? 16 : 64; }
 
 constexpr int attn_fwd_rows(int DP) { return 16 * kAttnWaves * attn_nq(DP); }
+// and the smaller tile of short grids (DP = 256: none)
+constexpr int attn_less_nq(int DP) { return DP == 256 ? 1 : attn_nq(DP) - 1; }
+constexpr int attn_less_rows(int DP) { return 16 * kAttnWaves * attn_less_nq(DP); }
 constexpr int attn_bwd_cols(int DP, bool KV) { return 16 * kAttnWaves * attn_nt(DP, KV); }
 
 template <typename K, typename A>
@@ -50,9 +53,10 @@ hipError_t launch(K kernel, int64_t grid, int threads, const A& args, hipStream_
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(threads), p, 0, st);
 }
 
-// rows: rows of a tile; at most rows_most(DP): k_attn_rows
+// rows: rows of a tile; few: k_attn_rows (16 or rows_most(DP)), else k_attn_fwd
+// (attn_fwd_rows(DP) or attn_less_rows(DP))
 template <typename T, int DP>
-hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int rows, int64_t grid, hipStream_t st);
+hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, bool few, int rows, int64_t grid, hipStream_t st);
 // cols: columns of a workgroup, attn_bwd_cols(DP, kv) or (dK and dV at DP = 128) half of them
 template <typename T, int DP>
 hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int cols, int64_t grid, hipStream_t st);
@@ -64,21 +68,26 @@ hipError_t attn_rows(const AttnFwdArgs& a, int64_t grid, hipStream_t st) {
   return launch(a.k.vec && a.v.vec ? &k_attn_rows<T, DP, NQ, NW, PAGED, true> : &k_attn_rows<T, DP, NQ, NW, PAGED, false>,
                 grid, 64 * NW, a, st);
 }
+template <typename T, int DP, int NQ>
+hipError_t attn_tiles(const AttnFwdArgs& a, bool paged, int64_t grid, hipStream_t st) {
+  constexpr int NW = kAttnWaves;
+  const bool wide = a.k.vec && a.v.vec;
+  return launch(paged ? wide ? &k_attn_fwd<T, DP, NQ, NW, true, true> : &k_attn_fwd<T, DP, NQ, NW, true, false>
+                : wide ? &k_attn_fwd<T, DP, NQ, NW, false, true>
+                       : &k_attn_fwd<T, DP, NQ, NW, false, false>,
+                grid, 64 * NW, a, st);
+}
 template <typename T, int DP>
-hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, int rows, int64_t grid, hipStream_t st) {
-  constexpr int NQ = attn_nq(DP), NW = kAttnWaves;
+hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, bool few, int rows, int64_t grid, hipStream_t st) {
   hipError_t e;
-  if (rows <= rows_most(DP)) {
+  if (few) {
     constexpr int MOST = rows_most(DP) / 16;
     e = rows == 16 ? paged ? attn_rows<T, DP, 1, true>(a, grid, st) : attn_rows<T, DP, 1, false>(a, grid, st)
         : paged    ? attn_rows<T, DP, MOST, true>(a, grid, st)
                    : attn_rows<T, DP, MOST, false>(a, grid, st);
   } else {
-    const bool wide = a.k.vec && a.v.vec;
-    e = launch(paged ? wide ? &k_attn_fwd<T, DP, NQ, NW, true, true> : &k_attn_fwd<T, DP, NQ, NW, true, false>
-               : wide ? &k_attn_fwd<T, DP, NQ, NW, false, true>
-                      : &k_attn_fwd<T, DP, NQ, NW, false, false>,
-               grid, 64 * NW, a, st);
+    e = rows == attn_less_rows(DP) ? attn_tiles<T, DP, attn_less_nq(DP)>(a, paged, grid, st)
+                                   : attn_tiles<T, DP, attn_nq(DP)>(a, paged, grid, st);
   }
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t units = (int64_t)(a.s.packed ? 1 : a.s.B) * a.s.M * a.s.Hq;
@@ -103,7 +112,7 @@ hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int cols, int64_t grid, hipSt
   return launch(&k_attn_sum<T>, (units + 3) / 4, 256, a, st);
 }
 #define GS_ATTN_INSTANCE(T, DP)                                                               \
-  template hipError_t attn_fwd<T, DP>(const AttnFwdArgs&, bool, int, int64_t, hipStream_t);   \
+  template hipError_t attn_fwd<T, DP>(const AttnFwdArgs&, bool, bool, int, int64_t, hipStream_t); \
   template hipError_t attn_bwd<T, DP>(const AttnBwdArgs&, bool, int, int64_t, hipStream_t);
 #if GS_PART == 1 || GS_PART == -1
 GS_ATTN_INSTANCE(F16, 64)
@@ -238,6 +247,7 @@ struct Carve {
 // How a forward call is laid out: rows of a tile, query heads packed into the rows
 // of a token, tiles and heads of the grid, parts of a row's keys, workspace.
 struct FwdPlan {
+  bool few;
   int rows;
   int64_t per, tiles, heads, splits, grid;
   float *part_o, *part_z;
@@ -254,15 +264,35 @@ FwdPlan fwd_plan(const gs_attention_problem& p, bool paged, int64_t keys, void* 
   // rows that share a key head: with the query heads of a token packed, keys and
   // values are read once for all of them
   const int64_t shared = (p.packed && p.B > 0 ? (p.M + p.B - 1) / p.B : p.M) * G;
-  const bool few = shared <= rows_most(DP);
+  const bool few = f.few = shared <= rows_most(DP);
   f.per = paged || few ? G : 1;
   f.rows = !few ? attn_fwd_rows(DP) : shared <= 16 ? 16 : rows_most(DP);
   f.tiles = tiles_of(p, p.M * f.per, f.rows);
   f.heads = (f.per > 1 || G == 1 ? p.Hkv : p.Hq) * B;
+  // Short grids take a smaller tile: a workgroup is sooner done with each 64 keys and
+  // the last round fuller.  D = 128, 192 rows -> 128, below two rounds of 512
+  // workgroups: 1000 causal tokens, 16 heads 40 -> 32 us; 4 x 2048, no mask 158 -> 146
+  // us; 8 packed sequences of 800 60 -> 56 us; 2 x 4096 causal 156 -> 159 us, and above
+  // two rounds 192 rows are 8 % faster.  D = 64, 128 rows -> 64, where that fills the
+  // GPU or the keys are too few to be cut: 4 x 512, 8 heads 16.1 -> 11.6 us; 2 x 2000
+  // 46 -> 30 us; but 4000 tokens of 4 heads, cut in four, 39 -> 43 us.  Not over pages:
+  // 2 chunks to 2048 tokens, 32 heads 156 -> 173 us.
+  if (!few && !paged && DP != 256) {
+    const int64_t less = tiles_of(p, p.M * f.per, attn_less_rows(DP)), full = f.tiles * f.heads;
+    if (DP == 128 ? full < 1024 : full < 512 && (less * f.heads >= 512 || keys < 1024)) {
+      f.rows = attn_less_rows(DP);
+      f.tiles = less;
+    }
+  }
   // With fewer workgroups than two a CU a row's keys are cut into parts, none
-  // shorter than 256 (512) keys.  Chunks of up to 512 tokens over 3000 to 12000 keys:
-  // 256 workgroups 408 us, 512 283 us, 768 307 us, 1024 299 us
-  const int64_t wgs = f.tiles * f.heads, want = 512, least = few ? kLeastPart : 512;
+  // shorter than 256 (512) keys.  Chunks over several long paged sequences, whose
+  // lengths differ, take twice as many to even out; the parts cost the same for
+  // short ones.  32 / 8 heads, D = 128, 512 -> 1024 workgroups: 4 chunks to 512 tokens
+  // over 3000 to 12000 keys 405 -> 286 and 405 -> 269 us, where the longest chunk has
+  // few tokens 272 -> 288 us; 8 to 256 over 2000 to 8000 276 -> 185 us; 2 to 2048 over
+  // 1000 to 4000 156 -> 189 us.  D = 64: 8 to 300 over 1000 to 4000 60 -> 46 us.
+  const bool uneven = paged && !few && p.B > 1 && keys >= 40 * DP;
+  const int64_t wgs = f.tiles * f.heads, want = uneven ? 1024 : 512, least = few ? kLeastPart : 512;
   f.splits = wgs > 0 && keys >= 2 * least
                  ? std::max<int64_t>(1, std::min({want / wgs, keys / least, (int64_t)kMostParts}))
                  : 1;
@@ -406,7 +436,7 @@ gs_status run_fwd(const gs_attention_problem* p, const gs_attention_array* q, co
   a.lse_sh = p->M;
   plan_args(f, *p, a);
   const hipError_t e = by_type(*p, [&](auto t, auto dp) {
-    return attn_fwd<decltype(t), decltype(dp)::value>(a, false, f.rows, f.grid, stream);
+    return attn_fwd<decltype(t), decltype(dp)::value>(a, false, f.few, f.rows, f.grid, stream);
   });
   return e == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
 }
@@ -557,7 +587,7 @@ gs_status run_paged(const gs_attention_problem* p, const gs_attention_array* q, 
   a.lse_sh = p->M * B;
   plan_args(f, *p, a);
   const hipError_t e = by_type(*p, [&](auto t, auto dp) {
-    return attn_fwd<decltype(t), decltype(dp)::value>(a, true, f.rows, f.grid, stream);
+    return attn_fwd<decltype(t), decltype(dp)::value>(a, true, f.few, f.rows, f.grid, stream);
   });
   return e == hipSuccess ? GS_SUCCESS : GS_ERR_HIP;
 }
