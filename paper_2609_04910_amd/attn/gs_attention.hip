@@ -647,7 +647,8 @@ gs_status gs_attention_bwd(const gs_attention_problem* p, const gs_attention_arr
                            const gs_attention_array* v, const int32_t* q_index, const int32_t* k_index,
                            const gs_attention_array* out, const gs_attention_array* low, const float* lse,
                            const gs_attention_array* dout, const gs_attention_array* dq,
-                           const gs_attention_array* dk, const gs_attention_array* dv, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+                           const gs_attention_array* dk, const gs_attention_array* dv, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream) {
   return gs::run_bwd(p, q, k, v, q_index, k_index, out, low, lse, dout, dq, dk, dv, workspace, workspace_bytes, stream);
 }
 
