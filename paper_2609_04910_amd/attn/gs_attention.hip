@@ -57,7 +57,7 @@ hipError_t launch(K kernel, int64_t grid, int threads, const A& args, hipStream_
 // (attn_fwd_rows(DP) or attn_less_rows(DP))
 template <typename T, int DP>
 hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, bool few, int rows, int64_t grid, hipStream_t st);
-// cols: columns of a workgroup, attn_bwd_cols(DP, kv) or (dK and dV at DP = 128) half of them
+// cols: columns of a workgroup, attn_bwd_cols(DP, kv) or (not DP = 256) half of them
 template <typename T, int DP>
 hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int cols, int64_t grid, hipStream_t st);
 
@@ -101,12 +101,12 @@ hipError_t attn_pass(const AttnBwdArgs& a, int64_t grid, hipStream_t st) {
 }
 template <typename T, int DP>
 hipError_t attn_bwd(const AttnBwdArgs& a, bool kv, int cols, int64_t grid, hipStream_t st) {
-  if (!kv) return attn_pass<T, DP, attn_nt(DP, false), false>(a, grid, st);
-  hipError_t e;
-  if (DP == 128 && cols < attn_bwd_cols(DP, true))
-    e = attn_pass<T, DP, DP == 128 ? 1 : attn_nt(DP, true), true>(a, grid, st);
-  else
-    e = attn_pass<T, DP, attn_nt(DP, true), true>(a, grid, st);
+  constexpr int LESS = DP == 256 ? attn_nt(DP, true) : 1;
+  const bool less = cols < attn_bwd_cols(DP, kv);
+  if (!kv)
+    return less ? attn_pass<T, DP, LESS, false>(a, grid, st) : attn_pass<T, DP, attn_nt(DP, false), false>(a, grid, st);
+  const hipError_t e =
+      less ? attn_pass<T, DP, LESS, true>(a, grid, st) : attn_pass<T, DP, attn_nt(DP, true), true>(a, grid, st);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t units = (int64_t)(a.s.packed ? 1 : a.s.B) * a.s.N * a.s.Hkv;
   return launch(&k_attn_sum<T>, (units + 3) / 4, 256, a, st);
@@ -320,7 +320,7 @@ void plan_args(const FwdPlan& f, const gs_attention_problem& p, AttnFwdArgs& a) 
 // How a backward call is laid out: columns of a workgroup of the dK, dV pass, the
 // grids of both passes, workgroups that share a key head's query heads, workspace.
 struct BwdPlan {
-  int k_cols;
+  int q_cols, k_cols;
   int64_t q_tiles, q_heads, k_tiles, k_heads, splits;
   float *norms, *delta, *lse2, *part;
   int64_t part_width;
@@ -331,18 +331,27 @@ BwdPlan bwd_plan(const gs_attention_problem& p, bool want_kv, void* ws) {
   BwdPlan f{};
   const int DP = padded_width(p.D, p.C);
   const int64_t B = p.packed ? 1 : p.B, G = p.Hq / p.Hkv;
-  f.q_tiles = tiles_of(p, p.M, attn_bwd_cols(DP, false)), f.q_heads = p.Hq * B;
+  f.q_heads = p.Hq * B;
+  f.q_cols = attn_bwd_cols(DP, false);
+  f.q_tiles = tiles_of(p, p.M, f.q_cols);
+  // dQ: tiles of half the columns where those of all leave less than two workgroups
+  // a CU.  1000 causal tokens, 16 heads, D = 128 42 -> 30 us; 4000, 8 heads 132 -> 98 us;
+  // 4 x 512, 8 heads, D = 64 22 -> 17 us; at 700 workgroups (6 packed to 2047) 74 -> 85 us
+  if (DP != 256 && f.q_tiles * f.q_heads < 512) {
+    f.q_cols /= 2;
+    f.q_tiles = tiles_of(p, p.M, f.q_cols);
+  }
   f.k_heads = p.Hkv * B;
   f.k_cols = attn_bwd_cols(DP, true);
   f.k_tiles = tiles_of(p, p.N, f.k_cols);
   // dK, dV: 512 workgroups fill the GPU (two a CU); with a causal mask, whose tiles
   // have unequal numbers of pairs, it takes 1024 to even out.  Where there are fewer
   // the query heads of a key head are shared by several workgroups, as far as they
-  // go (causal: to 2048, since the sums cost a pass anyway), and then at D = 128
+  // go (causal: to 2048, since the sums cost a pass anyway), and then (not D = 256)
   // tiles of half the columns are taken.  8192 tokens, 32 heads over 8, causal: 512
   // workgroups 1531 us, 1024 half tiles 1380 us, heads shared by two 1237 us, by
   // four 1181 us; 4 x 4096 tokens (1024 workgroups): not shared 1156 us, by two
-  // 1228 us.
+  // 1228 us.  Half tiles at D = 64: 2 x 2000 causal tokens, 8 heads 70 -> 52 us.
   const bool even = !p.causal || (p.window > 0 && 2 * p.window <= p.N) || (p.packed && p.B >= 4);
   const int64_t want = even ? 512 : 1024, wgs = f.k_tiles * f.k_heads;
   f.splits = 1;
@@ -351,7 +360,7 @@ BwdPlan bwd_plan(const gs_attention_problem& p, bool want_kv, void* ws) {
       do ++f.splits;
       while (G % f.splits);
     }
-  if (DP == 128 && f.k_tiles * f.k_heads * f.splits < want) {
+  if (DP != 256 && f.k_tiles * f.k_heads * f.splits < want) {
     f.k_cols /= 2;
     f.k_tiles = tiles_of(p, p.N, f.k_cols);
   }
@@ -516,7 +525,7 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
     a.wgs = a.tiles * a.heads;
     a.part = w.part, a.part_width = (int32_t)w.part_width;
     e = by_type(*p, [&](auto t, auto dp) {
-      return attn_bwd<decltype(t), decltype(dp)::value>(a, kv != 0, w.k_cols, (int64_t)a.wgs * a.splits, stream);
+      return attn_bwd<decltype(t), decltype(dp)::value>(a, kv != 0, kv ? w.k_cols : w.q_cols, (int64_t)a.wgs * a.splits, stream);
     });
     if (e != hipSuccess) return GS_ERR_HIP;
   }
