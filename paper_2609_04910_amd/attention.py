@@ -292,20 +292,21 @@ def _check_like_out(t, name, c, q):
 def _fwd(c, q, k, v, out, lse, low, workspace, stream):
     import torch
     rest = 0
-    if out is None:
-        rest = REST_OUT
-        out = torch.empty(c.out_shape, dtype=q.dtype, device=q.device)
-    else:
+    if out is not None:
         _check_like_out(out, "out", c, q)
-    if lse is None:
-        lse = torch.empty(c.lse_shape, dtype=torch.float32, device=q.device)
-        rest |= REST_LSE
-    else:
+    if lse is not None:
         gs._check_tensor(lse, "lse", c.lse_shape, q.device, torch.float32)
     need = _fwd_bytes(c.sizes, c.modes)
     wbytes = 0
-    if need or workspace is not None:
-        workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
+    with gs._on(stream):
+        if out is None:
+            rest = REST_OUT
+            out = torch.empty(c.out_shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty(c.lse_shape, dtype=torch.float32, device=q.device)
+            rest |= REST_LSE
+        if need or workspace is not None:
+            workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
     packed, index = c.packed, c.index
     buf, at = _buffer()
     _PACK_FWD(buf, 0, *c.sizes, *c.modes, rest, c.scale, *_numbers(q, packed), *_numbers(k, packed),
@@ -314,7 +315,7 @@ def _fwd(c, q, k, v, out, lse, low, workspace, stream):
     _launch("gs_attention_fwd", c.gpu, stream, at - _AT_ARRAYS, at, at + 32, at + 64, gs._ptr(index[0]),
             gs._ptr(index[1]), at + 96, None if low is None else at + 128, lse.data_ptr(), gs._ptr(workspace), wbytes)
     if stream is not None:
-        gs._keep_alive(stream, out, lse, workspace)
+        gs._keep_alive(stream, out, lse, workspace=workspace)
     return out, lse
 
 
@@ -348,10 +349,11 @@ def attention_bwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed
 def _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream):
     import torch
     want = int(bool(want[0])), int(bool(want[1])), int(bool(want[2]))
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want[0] else None
-    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if want[1] else None
-    dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if want[2] else None
-    workspace, wbytes = gs._workspace_arg(workspace, _bwd_bytes(c.sizes, c.modes, want), q.device)
+    with gs._on(stream):
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want[0] else None
+        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if want[1] else None
+        dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if want[2] else None
+        workspace, wbytes = gs._workspace_arg(workspace, _bwd_bytes(c.sizes, c.modes, want), q.device)
     packed, index = c.packed, c.index
     buf, at = _buffer()
     _PACK_BWD(buf, 0, *c.sizes, *c.modes, REST_OUT, c.scale, *_numbers(q, packed), *_numbers(k, packed),
@@ -363,7 +365,7 @@ def _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream):
             at + 192 if want[0] else None, at + 224 if want[1] else None, at + 256 if want[2] else None,
             gs._ptr(workspace), wbytes)
     if stream is not None:
-        gs._keep_alive(stream, workspace, dq, dk, dv)
+        gs._keep_alive(stream, dq, dk, dv, workspace=workspace)
     return dq, dk, dv
 
 
@@ -515,30 +517,30 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     C = v_pages.shape[3]
     sizes, modes = _cache_call(q, "q", k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window)
     _check_gpu(("q", q), ("k_pages", k_pages), ("v_pages", v_pages))
-    rest = 0
-    if out is None:
-        rest = REST_OUT
-        out = torch.empty((T, Hq, C), dtype=q.dtype, device=q.device)
-    else:
+    rest, lse, wbytes = 0, None, 0
+    if out is not None:
         _check_out(out, "out", (T, Hq, C), q.dtype, q.device)
         _check_columns("out", out, 3)
-    lse = None
-    if return_lse:
-        lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
-        rest |= REST_LSE
-    if sizes[0] == 0:  # no sequences: every row is one of none
-        with torch.cuda.stream(stream):
+    with gs._on(stream):
+        if out is None:
+            rest = REST_OUT
+            out = torch.empty((T, Hq, C), dtype=q.dtype, device=q.device)
+        if return_lse:
+            lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
+            rest |= REST_LSE
+        if sizes[0] == 0:  # no sequences: every row is one of none
             if rest & REST_OUT:
                 out.zero_()
             if lse is not None:
                 lse.fill_(float("-inf"))
+        else:
+            need = _paged_bytes(sizes, modes, k_pages.shape[1], page_table.shape[1])
+            if need or workspace is not None:
+                workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
+    if sizes[0] == 0:
         if stream is not None:
             gs._keep_alive(stream, out, lse)
         return (out, lse) if return_lse else out
-    need = _paged_bytes(sizes, modes, k_pages.shape[1], page_table.shape[1])
-    wbytes = 0
-    if need or workspace is not None:
-        workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
     buf, at = _buffer()
     _PACK_PAGED(buf, 0, *sizes, *modes, rest, D ** -0.5 if scale is None else float(scale),
                 *_row_numbers(q, sizes, modes), *_row_numbers(out, sizes, modes),
@@ -546,5 +548,5 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     _launch("gs_attention_paged", q.get_device(), stream, at, at + 88, at + 152, gs._ptr(q_offsets), at + 120,
             gs._ptr(lse), gs._ptr(workspace), wbytes)
     if stream is not None:
-        gs._keep_alive(stream, out, lse, workspace)
+        gs._keep_alive(stream, out, lse, workspace=workspace)
     return (out, lse) if return_lse else out

@@ -19,6 +19,7 @@ Entry points mirror the C names:
   gauss_sum_status_string / gauss_sum_abi_version
 and ``GaussSum`` wraps both in a torch.autograd.Function.
 """
+import contextlib
 import ctypes
 import os
 
@@ -276,19 +277,42 @@ def _stream(stream):
     return _stream_of(stream).cuda_stream
 
 
-def _keep_alive(stream, *tensors):
-    """Tensors allocated here on torch's current stream but used by kernels
-    enqueued on another `stream`: mark them as in use on that stream, so the
-    caching allocator does not hand their memory out again before those
-    kernels finish."""
-    if stream is None:
+_HERE = contextlib.nullcontext()
+
+
+def _is_current(stream):
+    """Whether `stream` is None or torch's current stream of its GPU (by the handles: Stream
+    objects take 3 us)."""
+    import torch
+    return stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(stream.device.index)
+
+
+def _on(stream):
+    """Context in which a call's results and workspace are allocated: `stream`'s own part
+    of the caching allocator.  Memory of torch's current stream may be a block whose last
+    owner is gone on the host but has work pending there, which would then run beside the
+    call's kernels on `stream`."""
+    if _is_current(stream):
+        return _HERE
+    import torch
+    return torch.cuda.stream(stream)
+
+
+def _keep_alive(stream, *results, workspace=None):
+    """After a call on another `stream` than torch's current one: results are marked as in
+    use on both (the call's kernels write them on `stream`, the caller's next work reads
+    them), the workspace on `stream`, so the caching allocator does not hand their memory
+    out again before that work finishes."""
+    if _is_current(stream):
         return
     import torch
-    if stream == torch.cuda.current_stream():
-        return
-    for t in tensors:
+    current = torch.cuda.current_stream(stream.device)
+    for t in results:
         if t is not None:
             t.record_stream(stream)
+            t.record_stream(current)
+    if workspace is not None:
+        workspace.record_stream(stream)
 
 
 def gauss_sum_fwd(q, k, v, tau, out=None, workspace=None, stream=None):

@@ -1,0 +1,80 @@
+"""Where the calls on a given stream allocate, without a GPU: results and workspace come from that
+stream's part of the caching allocator.  On the current stream's part they could be a block that work
+pending on the current stream still writes.  (Tensors are the CPU's, said to be on a GPU; the library is
+asked for sizes only.)"""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2609_04910_amd import attention as at
+from paper_2609_04910_amd import gauss_sum as gs
+
+H = torch.float16
+
+
+class Stream:
+    cuda_stream = 7
+    device = torch.device("cuda", 0)
+
+
+@pytest.fixture
+def where(monkeypatch):
+    """The handle of the stream on which each allocation was made, in turn."""
+    current, seen, empty = [0], [], torch.empty
+
+    @contextlib.contextmanager
+    def switch(stream):
+        before, current[0] = current[0], stream.cuda_stream
+        yield
+        current[0] = before
+
+    def allocate(*args, **kw):
+        seen.append(current[0])
+        return empty(*args, **kw)
+
+    real = gs.load()
+
+    class Sizes:
+        def __getattr__(self, name):
+            return getattr(real, name) if name.endswith("_size") else lambda *args: 0
+
+    monkeypatch.setattr(torch.cuda, "stream", switch)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *args: Stream())
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: current[0], raising=False)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda self: True))
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: None)
+    monkeypatch.setattr(torch, "empty", allocate)
+    monkeypatch.setattr(at, "_launch", lambda *args: None)
+    monkeypatch.setattr(gs, "load", lambda *args: Sizes())
+    return seen
+
+
+def z(*shape, dtype=H):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def i32(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+QKV = (z(1, 5, 2, 64), z(1, 5000, 2, 64), z(1, 5000, 2, 64))
+PAGES = (z(8, 64, 2, 64), z(8, 64, 2, 64))
+ATTENTION = {
+    "fwd": (lambda **kw: at.attention_fwd(*QKV, **kw), 3),
+    "bwd": (lambda **kw: at.attention_bwd(*QKV, QKV[0], torch.zeros(1, 2, 5), QKV[0], **kw), 4),
+    "paged": (lambda **kw: at.attention_paged(z(1, 2, 64), *PAGES, torch.zeros((1, 99), dtype=torch.int32), i32(9),
+                                              return_lse=True, **kw), 3),
+    "paged, no sequences": (lambda **kw: at.attention_paged(z(2, 2, 64), *PAGES, torch.zeros((0, 9), dtype=torch.int32),
+                                                            i32(), q_offsets=i32(0), return_lse=True, **kw), 2),
+}
+
+
+@pytest.mark.parametrize("name", ATTENTION)
+def test_attention_allocates_on_the_given_stream(where, name):
+    call, count = ATTENTION[name]
+    call(stream=Stream())
+    assert where == [7] * count
+    del where[:]
+    call()
+    assert where == [0] * count
