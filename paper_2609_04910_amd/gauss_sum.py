@@ -323,12 +323,13 @@ def gauss_sum_fwd(q, k, v, tau, out=None, workspace=None, stream=None):
     N, C = v.shape
     p = make_problem(M, N, D, C, _dtype_code(q.dtype), _dtype_code(v.dtype))
     lib = load()
-    out = _output(out, "out", (M, C), q.device)
     need = int(lib.gauss_sum_fwd_workspace_size(ctypes.byref(p)))
-    workspace, wbytes = _workspace_arg(workspace, need, q.device)
+    with _on(stream):
+        out = _output(out, "out", (M, C), q.device)
+        workspace, wbytes = _workspace_arg(workspace, need, q.device)
     st = lib.gauss_sum_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), float(tau), _ptr(out),
                            _ptr(workspace), wbytes, _stream(stream))
-    _keep_alive(stream, out, workspace)
+    _keep_alive(stream, out, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_fwd")
     return out
@@ -366,16 +367,17 @@ def gauss_sum_bwd(q, k, v, tau, dout, want=(True, True, True), workspace=None, s
     p = make_problem(M, N, D, C, _dtype_code(q.dtype), _dtype_code(v.dtype))
     lib = load()
     dev = q.device
-    dq = torch.empty((M, D), dtype=torch.float32, device=dev) if want[0] else None
-    dk = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
-    dv = torch.empty((N, C), dtype=torch.float32, device=dev) if want[2] else None
     need = int(lib.gauss_sum_bwd_workspace_size(ctypes.byref(p), int(bool(want[0])),
                                                 int(bool(want[1])), int(bool(want[2]))))
-    workspace, wbytes = _workspace_arg(workspace, need, dev)
+    with _on(stream):
+        dq = torch.empty((M, D), dtype=torch.float32, device=dev) if want[0] else None
+        dk = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
+        dv = torch.empty((N, C), dtype=torch.float32, device=dev) if want[2] else None
+        workspace, wbytes = _workspace_arg(workspace, need, dev)
     st = lib.gauss_sum_bwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), float(tau), _ptr(dout),
                            _dtype_code(dout.dtype), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
                            wbytes, _stream(stream))
-    _keep_alive(stream, dq, dk, dv, workspace)
+    _keep_alive(stream, dq, dk, dv, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_bwd")
     return dq, dk, dv
@@ -393,17 +395,18 @@ def gauss_sum_fwd_bwd(q, k, v, tau, dout, want=(True, True, True), out=None, wor
     p = make_problem(M, N, D, C, _dtype_code(q.dtype), _dtype_code(v.dtype))
     lib = load()
     dev = q.device
-    out = _output(out, "out", (M, C), dev)
-    dq = torch.empty((M, D), dtype=torch.float32, device=dev) if want[0] else None
-    dk = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
-    dv = torch.empty((N, C), dtype=torch.float32, device=dev) if want[2] else None
     need = int(lib.gauss_sum_fwd_bwd_workspace_size(ctypes.byref(p), int(bool(want[0])),
                                                     int(bool(want[1])), int(bool(want[2]))))
-    workspace, wbytes = _workspace_arg(workspace, need, dev)
+    with _on(stream):
+        out = _output(out, "out", (M, C), dev)
+        dq = torch.empty((M, D), dtype=torch.float32, device=dev) if want[0] else None
+        dk = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
+        dv = torch.empty((N, C), dtype=torch.float32, device=dev) if want[2] else None
+        workspace, wbytes = _workspace_arg(workspace, need, dev)
     st = lib.gauss_sum_fwd_bwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), float(tau), _ptr(dout),
                                _dtype_code(dout.dtype), _ptr(out), _ptr(dq), _ptr(dk), _ptr(dv),
                                _ptr(workspace), wbytes, _stream(stream))
-    _keep_alive(stream, out, dq, dk, dv, workspace)
+    _keep_alive(stream, out, dq, dk, dv, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_fwd_bwd")
     return out, dq, dk, dv
@@ -455,13 +458,14 @@ def gauss_sum_fwd_batched(q, k, v, tau, out=None, workspace=None, stream=None, g
     B, M, N, D, C, qs, ks, vs = _batched_inputs(q, k, v)
     p = make_problem(M, N, D, C, _dtype_code(q.dtype), _dtype_code(v.dtype))
     lib = load()
-    out = _output(out, "out", (B, M, C), q.device)
     b = Batch(B, qs, ks, vs, 0, M * C, 0, 0, 0)
     need = int(lib.gauss_sum_fwd_batched_workspace_size(ctypes.byref(p), int(group or max(B, 1))))
-    workspace, wbytes = _workspace_arg(workspace, need, q.device)
+    with _on(stream):
+        out = _output(out, "out", (B, M, C), q.device)
+        workspace, wbytes = _workspace_arg(workspace, need, q.device)
     st = lib.gauss_sum_fwd_batched(ctypes.byref(p), ctypes.byref(b), _ptr(q), _ptr(k), _ptr(v),
                                    float(tau), _ptr(out), _ptr(workspace), wbytes, _stream(stream))
-    _keep_alive(stream, out, workspace)
+    _keep_alive(stream, out, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_fwd_batched")
     return out
@@ -481,18 +485,19 @@ def gauss_sum_bwd_batched(q, k, v, tau, dout, want=(True, True, True), workspace
     p = make_problem(M, N, D, C, _dtype_code(q.dtype), _dtype_code(v.dtype))
     lib = load()
     dev = q.device
-    dq = torch.empty((B, M, D), dtype=torch.float32, device=dev) if want[0] else None
-    dk = torch.empty((B, N, D), dtype=torch.float32, device=dev) if want[1] else None
-    dv = torch.empty((B, N, C), dtype=torch.float32, device=dev) if want[2] else None
     b = Batch(B, qs, ks, vs, M * C, 0, M * D, N * D, N * C)
     need = int(lib.gauss_sum_bwd_batched_workspace_size(ctypes.byref(p), int(group or max(B, 1)),
                                                         int(bool(want[0])), int(bool(want[1])),
                                                         int(bool(want[2]))))
-    workspace, wbytes = _workspace_arg(workspace, need, dev)
+    with _on(stream):
+        dq = torch.empty((B, M, D), dtype=torch.float32, device=dev) if want[0] else None
+        dk = torch.empty((B, N, D), dtype=torch.float32, device=dev) if want[1] else None
+        dv = torch.empty((B, N, C), dtype=torch.float32, device=dev) if want[2] else None
+        workspace, wbytes = _workspace_arg(workspace, need, dev)
     st = lib.gauss_sum_bwd_batched(ctypes.byref(p), ctypes.byref(b), _ptr(q), _ptr(k), _ptr(v),
                                    float(tau), _ptr(dout), _dtype_code(dout.dtype), _ptr(dq), _ptr(dk),
                                    _ptr(dv), _ptr(workspace), wbytes, _stream(stream))
-    _keep_alive(stream, dq, dk, dv, workspace)
+    _keep_alive(stream, dq, dk, dv, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_bwd_batched")
     return dq, dk, dv
@@ -519,20 +524,21 @@ def gauss_sum_fwd_bwd_batched(q, k, v, tau, dout, want=(True, True, True), out=N
     p = make_problem(M, N, D, C, _dtype_code(q.dtype), _dtype_code(v.dtype))
     lib = load()
     dev = q.device
-    out = _output(out, "out", (B, M, C), dev)
-    dq = torch.empty((B, M, D), dtype=torch.float32, device=dev) if want[0] else None
-    dk = torch.empty((B, N, D), dtype=torch.float32, device=dev) if want[1] else None
-    dv = torch.empty((B, N, C), dtype=torch.float32, device=dev) if want[2] else None
     b = Batch(B, qs, ks, vs, M * C, M * C, M * D, N * D, N * C)
     need = int(lib.gauss_sum_fwd_bwd_batched_workspace_size(ctypes.byref(p), int(group or max(B, 1)),
                                                             int(bool(want[0])), int(bool(want[1])),
                                                             int(bool(want[2]))))
-    workspace, wbytes = _workspace_arg(workspace, need, dev)
+    with _on(stream):
+        out = _output(out, "out", (B, M, C), dev)
+        dq = torch.empty((B, M, D), dtype=torch.float32, device=dev) if want[0] else None
+        dk = torch.empty((B, N, D), dtype=torch.float32, device=dev) if want[1] else None
+        dv = torch.empty((B, N, C), dtype=torch.float32, device=dev) if want[2] else None
+        workspace, wbytes = _workspace_arg(workspace, need, dev)
     st = lib.gauss_sum_fwd_bwd_batched(ctypes.byref(p), ctypes.byref(b), _ptr(q), _ptr(k), _ptr(v),
                                        float(tau), _ptr(dout), _dtype_code(dout.dtype), _ptr(out),
                                        _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace), wbytes,
                                        _stream(stream))
-    _keep_alive(stream, out, dq, dk, dv, workspace)
+    _keep_alive(stream, out, dq, dk, dv, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_fwd_bwd_batched")
     return out, dq, dk, dv
@@ -555,14 +561,15 @@ def gauss_sum_mmd_flow(x, v, tau, want=(True, True, True), workspace=None, strea
     p = make_problem(N, N, D, 1, _dtype_code(x.dtype), _dtype_code(v.dtype))
     lib = load()
     dev = x.device
-    s = torch.empty((N, 1), dtype=torch.float32, device=dev) if want[0] else None
-    grad = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
-    mmd2 = torch.empty((), dtype=torch.float64, device=dev) if want[2] else None
     need = int(lib.gauss_sum_mmd_flow_workspace_size(ctypes.byref(p)))
-    workspace, wbytes = _workspace_arg(workspace, need, dev)
+    with _on(stream):
+        s = torch.empty((N, 1), dtype=torch.float32, device=dev) if want[0] else None
+        grad = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
+        mmd2 = torch.empty((), dtype=torch.float64, device=dev) if want[2] else None
+        workspace, wbytes = _workspace_arg(workspace, need, dev)
     st = lib.gauss_sum_mmd_flow(ctypes.byref(p), _ptr(x), _ptr(v), float(tau), _ptr(s), _ptr(grad),
                                 _ptr(mmd2), _ptr(workspace), wbytes, _stream(stream))
-    _keep_alive(stream, s, grad, mmd2, workspace)
+    _keep_alive(stream, s, grad, mmd2, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_mmd_flow")
     return s, grad, mmd2
@@ -585,12 +592,13 @@ def gauss_sum_svgd(x, score, tau, out=None, workspace=None, stream=None):
     p = make_problem(N, N, D, D, _dtype_code(x.dtype), _dtype_code(score.dtype))
     lib = load()
     dev = x.device
-    out = _output(out, "out", (N, D), dev)
     need = int(lib.gauss_sum_svgd_workspace_size(ctypes.byref(p)))
-    workspace, wbytes = _workspace_arg(workspace, need, dev)
+    with _on(stream):
+        out = _output(out, "out", (N, D), dev)
+        workspace, wbytes = _workspace_arg(workspace, need, dev)
     st = lib.gauss_sum_svgd(ctypes.byref(p), _ptr(x), _ptr(score), float(tau), _ptr(out), _ptr(workspace),
                             wbytes, _stream(stream))
-    _keep_alive(stream, out, workspace)
+    _keep_alive(stream, out, workspace=workspace)
     if st != 0:
         raise GaussSumError(st, "gauss_sum_svgd")
     return out

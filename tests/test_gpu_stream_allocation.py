@@ -59,3 +59,17 @@ def test_attention_over_pages():
     out, lse = at.attention_paged(q, kp, vp, table[:0], lens[:0], q_offsets=none, return_lse=True)
     assert not out.any() and (lse == -math.inf).all()
     run(lambda st: at.attention_paged(q, kp, vp, table[:0], lens[:0], q_offsets=none, return_lse=True, stream=st))
+
+
+def test_gauss_sums():
+    from paper_2609_04910_amd import gauss_sum as gs
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v, g = (torch.randn(s, generator=gen, device="cuda") for s in ((700, 32), (900, 32), (900, 4), (700, 4)))
+    q, k, weights = q.half(), k.half(), v[:, :1].contiguous()
+    run(lambda st: [gs.gauss_sum_fwd(q, k, v, 0.1, stream=st)], gs.gauss_sum_fwd_workspace_size(700, 900, 32, 4))
+    run(lambda st: gs.gauss_sum_bwd(q, k, v, 0.1, g, stream=st), gs.gauss_sum_bwd_workspace_size(700, 900, 32, 4))
+    run(lambda st: gs.gauss_sum_fwd_bwd(q, k, v, 0.1, g, stream=st), gs.gauss_sum_fwd_bwd_workspace_size(700, 900, 32, 4))
+    run(lambda st: gs.gauss_sum_mmd_flow(k, weights, 0.1, stream=st), gs.gauss_sum_mmd_flow_workspace_size(900, 32))
+    batched = [t.expand(3, -1, -1).contiguous() for t in (q, k, v, g)]
+    run(lambda st: gs.gauss_sum_fwd_bwd_batched(*batched[:3], 0.1, batched[3], stream=st),
+        gs.gauss_sum_fwd_bwd_batched_workspace_size(700, 900, 32, 4, 3))

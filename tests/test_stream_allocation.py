@@ -15,7 +15,7 @@ H = torch.float16
 
 class Stream:
     cuda_stream = 7
-    device = torch.device("cuda", 0)
+    device = torch.device("cpu")               # the tensors'
 
 
 @pytest.fixture
@@ -40,6 +40,7 @@ def where(monkeypatch):
             return getattr(real, name) if name.endswith("_size") else lambda *args: 0
 
     monkeypatch.setattr(torch.cuda, "stream", switch)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *args: Stream())
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: current[0], raising=False)
     monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda self: True))
@@ -78,3 +79,27 @@ def test_attention_allocates_on_the_given_stream(where, name):
     del where[:]
     call()
     assert where == [0] * count
+
+
+X, V = z(40, 16), torch.zeros(40, 3)
+XB, VB = z(2, 40, 16), torch.zeros(2, 40, 3)
+GAUSS = {
+    "fwd": lambda **kw: gs.gauss_sum_fwd(X, X, V, 1.0, **kw),
+    "bwd": lambda **kw: gs.gauss_sum_bwd(X, X, V, 1.0, V, **kw),
+    "fwd_bwd": lambda **kw: gs.gauss_sum_fwd_bwd(X, X, V, 1.0, V, **kw),
+    "fwd_batched": lambda **kw: gs.gauss_sum_fwd_batched(XB, XB, VB, 1.0, **kw),
+    "bwd_batched": lambda **kw: gs.gauss_sum_bwd_batched(XB, XB, VB, 1.0, VB, **kw),
+    "fwd_bwd_batched": lambda **kw: gs.gauss_sum_fwd_bwd_batched(XB, XB, VB, 1.0, VB, **kw),
+    "mmd_flow": lambda **kw: gs.gauss_sum_mmd_flow(X, V[:, :1].contiguous(), 1.0, **kw),
+    "svgd": lambda **kw: gs.gauss_sum_svgd(X, torch.zeros(40, 16), 1.0, **kw),
+}
+
+
+@pytest.mark.parametrize("name", GAUSS)
+def test_gauss_sums_allocate_on_the_given_stream(where, name):
+    GAUSS[name](stream=Stream())
+    assert where and set(where) == {7}
+    n = len(where)
+    del where[:]
+    GAUSS[name]()
+    assert where == [0] * n
