@@ -197,6 +197,12 @@ def _check_call(q, k, v, causal, window, q_offsets, k_offsets, q_lens, k_lens):
     _check_gpu(("q", q), ("k", k), ("v", v))
 
 
+def _check_stream(stream, device):
+    """A kernel enqueued on another GPU's stream would run there, on this one's addresses."""
+    if stream is not None and stream.device != device:
+        raise ValueError("stream must be on %s, got one on %s" % (device, stream.device))
+
+
 class _Call:
     """Checked sizes of a forward or backward call."""
     __slots__ = ("sizes", "modes", "scale", "packed", "index", "out_shape", "lse_shape", "gpu")
@@ -291,6 +297,7 @@ def _check_like_out(t, name, c, q):
 
 def _fwd(c, q, k, v, out, lse, low, workspace, stream):
     import torch
+    _check_stream(stream, q.device)
     rest = 0
     if out is not None:
         _check_like_out(out, "out", c, q)
@@ -348,6 +355,7 @@ def attention_bwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed
 
 def _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream):
     import torch
+    _check_stream(stream, q.device)
     want = int(bool(want[0])), int(bool(want[1])), int(bool(want[2]))
     with gs._on(stream):
         dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want[0] else None
@@ -490,6 +498,7 @@ def attention_append(k, v, k_pages, v_pages, page_table, seq_lens, q_offsets=Non
     if sizes[4] != H:
         raise ValueError("k has %d heads, the pages have %d" % (H, sizes[4]))
     _check_gpu(("k", k), ("v", v), ("k_pages", k_pages), ("v_pages", v_pages))
+    _check_stream(stream, k.device)
     buf, at = _buffer()
     _PACK_PAGED(buf, 0, *sizes, *modes, 0, 1.0, *_row_numbers(k, sizes, modes), *_row_numbers(v, sizes, modes),
                 *_cache_numbers(k_pages, v_pages, page_table, seq_lens))
@@ -517,6 +526,7 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     C = v_pages.shape[3]
     sizes, modes = _cache_call(q, "q", k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window)
     _check_gpu(("q", q), ("k_pages", k_pages), ("v_pages", v_pages))
+    _check_stream(stream, q.device)
     rest, lse, wbytes = 0, None, 0
     if out is not None:
         _check_out(out, "out", (T, Hq, C), q.dtype, q.device)

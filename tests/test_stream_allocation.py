@@ -103,3 +103,14 @@ def test_gauss_sums_allocate_on_the_given_stream(where, name):
     del where[:]
     GAUSS[name]()
     assert where == [0] * n
+
+
+def test_attention_refuses_a_stream_of_another_gpu(where):
+    other = Stream()
+    other.device = torch.device("cuda", 1)
+    table, lens = torch.zeros((1, 9), dtype=torch.int32), i32(9)
+    for call in [call for call, _ in ATTENTION.values()] + [
+            lambda **kw: at.attention_append(z(1, 2, 64), z(1, 2, 64), *PAGES, table, lens, **kw)]:
+        with pytest.raises(ValueError, match="stream must be on"):
+            call(stream=other)
+    assert not where
