@@ -745,8 +745,10 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
 #pragma unroll 8
   for (int p0 = 0; p0 < a.splits; p0 += groups) {
     const int p = p0 + group;
-    const float wp = __shfl(w, p & 63);
-    if (p >= a.splits || c >= s.C || wp == 0.0f) continue;  // (parts without keys hold no sums)
+    const float wp = __shfl(w, p & 63), op = __shfl(off, p & 63);
+    // parts without keys hold no sums; one whose weight vanishes beside the others'
+    // still counts: its sums may hold an infinity or NaN, and 0 times those is NaN
+    if (p >= a.splits || c >= s.C || op == kNoOffset) continue;
     y += load_sums(a.part_o + (p * units + unit) * s.C, c, s.C) * wp;
   }
   for (int d = span; d < 64; d <<= 1)

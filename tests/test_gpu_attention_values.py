@@ -1,0 +1,66 @@
+"""Softmax attention on the GPU at values where a result depends on more than the pairs it sums: values
+and gradients that are not finite, scores that are all -inf, numbers at the border of fp16, sequences
+whose gradients lie far apart.  Against 64 bits (attention_ref.one) and the rule that NaN and infinity
+reach the rows that see them and no other."""
+import math
+
+import pytest
+import torch
+
+import attention_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def at():
+    from paper_2609_04910_amd import attention
+    attention.load()
+    return attention
+
+
+def normal(gen, shape, dtype, std=1.0):
+    return (torch.randn(shape, generator=gen, dtype=torch.float64) * std).to(dtype).cuda()
+
+
+def make(seed, B, M, N, Hq, Hkv, D, C, dtype, std=1.0, g_std=0.1):
+    gen = torch.Generator().manual_seed(seed)
+    return (normal(gen, (B, M, Hq, D), dtype, std), normal(gen, (B, N, Hkv, D), dtype),
+            normal(gen, (B, N, Hkv, C), dtype), normal(gen, (B, M, Hq, C), dtype, g_std))
+
+
+def paged_of(k, v, page=16):
+    """One sequence's keys and values (n x H x width) as a cache: pages in descending order."""
+    n = k.shape[0]
+    pages = -(-n // page)
+    table = torch.arange(pages - 1, -1, -1, dtype=torch.int32, device="cuda")[None].contiguous()
+    out = []
+    for t in (k, v):
+        p = torch.zeros((pages, page) + t.shape[1:], dtype=t.dtype, device="cuda")
+        whole = torch.cat([t, t.new_zeros((pages * page - n,) + t.shape[1:])]).view((pages, page) + t.shape[1:])
+        p[table[0].long()] = whole
+        out.append(p)
+    return out[0], out[1], table, torch.tensor([n], dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("M,N", [(1, 5000), (200, 3000)])
+def test_a_bad_value_of_vanishing_weight_in_a_part_of_its_own(at, M, N, bad, dtype):
+    """The keys are cut into parts, and those of the last third score so low that their weights are 0 beside the
+    others': a value there that is not finite still reaches every row (0 times it is NaN), in its column only."""
+    q, k, v, _ = make(40, 1, M, N, 1, 1, 64, 64, dtype)
+    q[..., 0], k[..., 0] = 8.0, 0.0
+    k[:, 2 * N // 3:, :, 0] = -60.0           # scores below the others by 8 * 60
+    assert at.attention_fwd_workspace_size(1, M, N, 1, 1, 64, 64) > 0
+    clean = at.attention_fwd(q, k, v, scale=1.0)
+    v[0, N - 300, 0, 5] = bad
+    out, lse = at.attention_fwd(q, k, v, scale=1.0)
+    cache = paged_of(k[0], v[0])
+    paged = at.attention_paged(q[0], *cache, scale=1.0)
+    others = torch.arange(64, device="cuda") != 5
+    # the last row of a chunk sees every key; the rows before it lack keys behind the bad one
+    for o in (out[0], paged):
+        assert not o[..., 5].isfinite().any()
+        assert o[..., others].isfinite().all()
+    assert torch.equal(out[..., others], clean[0][..., others]) and torch.equal(lse, clean[1])
