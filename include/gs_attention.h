@@ -25,7 +25,8 @@
  * Rows see:  all keys of their sequence; with `causal`, row i of qn sees keys
  * j <= i + kn - qn (the last row sees every key), and with window > 0 only the
  * last `window` of those.  A row that sees nothing gives out = 0, lse = -inf and
- * no gradient.
+ * no gradient.  (One that sees keys whose scores are all -inf is another matter:
+ * out is 0 / 0 = NaN, lse log 0 = -inf.)
  *
  * Memory and ownership
  *   - Data pointers are DEVICE pointers owned by the caller.  Arrays are given by

@@ -44,7 +44,7 @@ struct AttnFwdArgs {
   int32_t wgs;             // workgroups of one part
   int32_t splits;          // parts that a row's keys are cut into (1: results are written at once)
   float* part_o;           // splits x rows x query heads x C: sums of weights times values
-  float* part_z;           // splits x rows x query heads x 2: offset and sum of weights
+  float* part_z;           // splits x rows x query heads x 2: offset (or kNoKeys) and sum of weights
 };
 
 // Weights lie below 2^15 relative to the offset, the largest of a row between
@@ -54,6 +54,9 @@ struct AttnFwdArgs {
 constexpr float kOffsetBelow = 7.0f;
 constexpr float kOffsetLimit = 15.0f;
 constexpr float kNoOffset = -3.0e38f;
+// Offset of a part that holds no key of the row (one whose scores are all -inf keeps
+// kNoOffset: the row is no empty one, and its result is 0 / 0).
+constexpr float kNoKeys = -__builtin_inff();
 
 __device__ __forceinline__ int page_index(const AttnPages& pg, int j) {
   return pg.shift >= 0 ? j >> pg.shift : (int)((uint32_t)j / (uint32_t)pg.size);
@@ -449,14 +452,17 @@ struct AttnRows {
     }
   }
   int max_key;  // the last key whose page number is at hand
+
+  // Whether the row of column tile n sees any of the keys [from, to).
+  __device__ __forceinline__ bool sees(int n, int from, int to) const { return max(lo[n], from) < min(hi[n], to); }
 };
 
-// Results of columns c .. c + 3 of row r (o / sum of weights z, offset off; first:
-// the thread that writes the row's own numbers): to the caller's arrays, or as
-// part of a row whose keys are split.
+// Results of columns c .. c + 3 of row r (o / sum of weights z, offset off; seen: the
+// row sees keys here; first: the thread that writes the row's own numbers): to the
+// caller's arrays, or as part of a row whose keys are split.
 template <typename T>
 __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w, int r, int c, floatx4 o, float off,
-                                          float z, bool first) {
+                                          float z, bool seen, bool first) {
   const AttnShape& s = a.s;
   if (r >= w.limit) return;
   const bool rest = r >= w.rows;
@@ -466,12 +472,12 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
   const int64_t row = w.sq.q0 + token;
   if (a.splits > 1) {
     const int64_t at = ((w.part * (int64_t)(s.packed ? 1 : s.B) + (s.packed ? 0 : w.b)) * s.M + row) * s.Hq + h;
-    if (first) a.part_z[2 * at] = off, a.part_z[2 * at + 1] = z;
-    if (off == kNoOffset) return;  // no keys: the sums are not looked at
+    if (first) a.part_z[2 * at] = seen ? off : kNoKeys, a.part_z[2 * at + 1] = z;
+    if (!seen) return;  // the sums are not looked at
     store_sums(a.part_o + at * s.C, c, s.C, o);
     return;
   }
-  const bool empty = rest || z == 0.0f;
+  const bool empty = rest || !seen;
   const float inv = 1.0f / z;
   floatx4 y;
 #pragma unroll
@@ -577,7 +583,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
       floatx4 y = rows.o[ct][n];
       if (infinities) add_infinities<NB>(inf_bits[threadIdx.x], n, ct, y);
       write_row<T>(a, job, wr0 + 16 * n + (lane & 15), 16 * ct + 4 * (lane >> 4), y, rows.off[n], z,
-                   ct == 0 && lane < 16);
+                   rows.sees(n, k_lo, k_hi), ct == 0 && lane < 16);
     }
   }
 }
@@ -594,6 +600,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
   __shared__ uint32_t inf_bits[NT][2 * NQ * NB];
   __shared__ int32_t slice[PAGED ? kSlice : 1];
   __shared__ float w_off[NW][ROWS], w_sum[NW][ROWS];
+  __shared__ bool seen[ROWS];
   const AttnShape& s = a.s;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 
@@ -664,6 +671,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
     z += __shfl_xor(z, 16);
     z += __shfl_xor(z, 32);
     if (lane < 16) w_off[wave][16 * n + lane] = rows.off[n], w_sum[wave][16 * n + lane] = z;
+    if (threadIdx.x < 16) seen[16 * n + lane] = rows.sees(n, k_lo, k_hi);
   }
   __syncthreads();  // also: every wave is done with its ring
   floatx4* join = reinterpret_cast<floatx4*>(smem);
@@ -692,7 +700,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
       z += w_sum[w][r] * __builtin_amdgcn_exp2f(w_off[w][r] - top);
       y += join[w * NQ * NO * 64 + i];
     }
-    write_row<T>(a, job, job.r0 + r, 16 * ct + 4 * (l >> 4), y, top, z, ct == 0 && l < 16);
+    write_row<T>(a, job, job.r0 + r, 16 * ct + 4 * (l >> 4), y, top, z, seen[r], ct == 0 && l < 16);
   }
 }
 
@@ -725,7 +733,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
     if (lse && lane == 0 && (s.zero_rest & kRestLse)) *lse = -__builtin_inff();
     return;
   }
-  float off = kNoOffset, z = 0.0f;
+  float off = kNoKeys, z = 0.0f;
   if (lane < a.splits) {
     const floatx2 p = *reinterpret_cast<const floatx2*>(a.part_z + 2 * (lane * units + unit));
     off = p[0], z = p[1];
@@ -737,7 +745,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
   z *= w;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) z += __shfl_xor(z, d);
-  const bool empty = z == 0.0f;
+  const bool empty = top == kNoKeys;
   const float inv = 1.0f / z;
   const int span = s.C > 128 ? 64 : s.C > 64 ? 32 : 16, groups = 64 / span, group = lane / span;
   const int c = 4 * (lane & (span - 1));
@@ -748,7 +756,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
     const float wp = __shfl(w, p & 63), op = __shfl(off, p & 63);
     // parts without keys hold no sums; one whose weight vanishes beside the others'
     // still counts: its sums may hold an infinity or NaN, and 0 times those is NaN
-    if (p >= a.splits || c >= s.C || op == kNoOffset) continue;
+    if (p >= a.splits || c >= s.C || op == kNoKeys) continue;
     y += load_sums(a.part_o + (p * units + unit) * s.C, c, s.C) * wp;
   }
   for (int d = span; d < 64; d <<= 1)

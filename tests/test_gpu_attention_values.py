@@ -64,3 +64,34 @@ def test_a_bad_value_of_vanishing_weight_in_a_part_of_its_own(at, M, N, bad, dty
         assert not o[..., 5].isfinite().any()
         assert o[..., others].isfinite().all()
     assert torch.equal(out[..., others], clean[0][..., others]) and torch.equal(lse, clean[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M,N", [(5, 70), (130, 90), (5, 3000), (200, 3000)])
+def test_rows_whose_scores_are_all_minus_infinity(at, M, N, dtype):
+    """They see keys, so they are no empty rows: 0 / 0 is NaN (lse: log 0).  In one part and in several."""
+    q, k, v, _ = make(45, 2, M, N, 2, 1, 64, 64, dtype)
+    k[..., 0] = k[..., 0].abs() + 1
+    clean = at.attention_fwd(q, k, v)
+    q[1, 3, 0, 0] = -math.inf
+    out, lse = at.attention_fwd(q, k, v)
+    assert out[1, 3, 0].isnan().all() and lse[1, 0, 3] == -math.inf
+    out[1, 3, 0], lse[1, 0, 3] = clean[0][1, 3, 0], clean[1][1, 0, 3]
+    assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
+    paged, plse = at.attention_paged(q[1], *paged_of(k[1], v[1]), return_lse=True)
+    assert (paged[3, 0].isnan().all() if M <= N else not paged[3, 0].any()) and plse[0, 3] == -math.inf
+    assert paged[:3].isfinite().all() and paged[4:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M", [20, 150])
+def test_a_first_key_of_minus_infinity(at, M, dtype):
+    """Causal: the first row sees that key alone (NaN), the others as if it were not there."""
+    q, k, v, _ = make(46, 1, M, M, 1, 1, 64, 64, dtype)
+    q[..., 0] = q[..., 0].abs() + 1
+    k[0, 0, 0, 0] = -math.inf
+    out, lse = at.attention_fwd(q, k, v, causal=True)
+    assert out[0, 0].isnan().all() and lse[0, 0, 0] == -math.inf
+    r = ref.one(q[0, 1:], k[0, 1:], v[0, 1:], 0.125, True)
+    ref.check("out", out[0, 1:], *r["out"])
+    ref.check("lse", lse[0, :, 1:], *r["lse"])
