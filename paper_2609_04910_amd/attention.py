@@ -305,7 +305,7 @@ def _fwd(c, q, k, v, out, lse, low, workspace, stream):
         gs._check_tensor(lse, "lse", c.lse_shape, q.device, torch.float32)
     need = _fwd_bytes(c.sizes, c.modes)
     wbytes = 0
-    with gs._on(stream):
+    with gs._HERE if stream is None else gs._on(stream):
         if out is None:
             rest = REST_OUT
             out = torch.empty(c.out_shape, dtype=q.dtype, device=q.device)
@@ -357,7 +357,7 @@ def _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream):
     import torch
     _check_stream(stream, q.device)
     want = int(bool(want[0])), int(bool(want[1])), int(bool(want[2]))
-    with gs._on(stream):
+    with gs._HERE if stream is None else gs._on(stream):
         dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want[0] else None
         dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if want[1] else None
         dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if want[2] else None
@@ -531,7 +531,7 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     if out is not None:
         _check_out(out, "out", (T, Hq, C), q.dtype, q.device)
         _check_columns("out", out, 3)
-    with gs._on(stream):
+    with gs._HERE if stream is None else gs._on(stream):
         if out is None:
             rest = REST_OUT
             out = torch.empty((T, Hq, C), dtype=q.dtype, device=q.device)

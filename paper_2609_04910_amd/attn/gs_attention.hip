@@ -322,7 +322,7 @@ void plan_args(const FwdPlan& f, const gs_attention_problem& p, AttnFwdArgs& a) 
 struct BwdPlan {
   int q_cols, k_cols;
   int64_t q_tiles, q_heads, k_tiles, k_heads, splits;
-  float *norms, *delta, *lse2, *part;
+  float *delta, *lse2, *part;
   int64_t part_width;
   size_t total;
 };
@@ -365,7 +365,6 @@ BwdPlan bwd_plan(const gs_attention_problem& p, bool want_kv, void* ws) {
     f.k_tiles = tiles_of(p, p.N, f.k_cols);
   }
   Carve c{static_cast<char*>(ws)};
-  f.norms = c.take<float>(2 * kNormBlocks);
   f.delta = c.take<float>(row_heads(p));
   f.lse2 = c.take<float>(row_heads(p));
   f.part_width = 2 * ((std::max(p.D, p.C) + 3) / 4 * 4);
@@ -491,28 +490,19 @@ gs_status run_bwd(const gs_attention_problem* p, const gs_attention_array* q, co
   a.st_sb = p->packed ? 0 : p->Hq * p->M;
   a.st_sh = p->M;
   a.c = p->scale * kLog2e;
-  const bool scaling = p->dtype == GS_F16;
-  a.norms = scaling ? w.norms : nullptr;
 
   AttnPrepArgs pr{};
   pr.s = a.s;
-  pr.out = ao, pr.low = alow, pr.dout = a.dout, pr.v = a.v;
+  pr.out = ao, pr.low = alow, pr.dout = a.dout;
   pr.lse = lse;
   pr.lse2 = w.lse2;
   pr.delta = w.delta;
   pr.st_sb = a.st_sb, pr.st_sh = a.st_sh;
-  pr.norms = scaling ? w.norms : nullptr;
-  pr.q_units = row_heads(*p);
-  pr.k_units = scaling ? B * p->N * p->Hkv : 0;
-  // enough workgroups to fill the GPU several times; with norms as many as the
-  // passes read maxima of
-  const int64_t most = scaling ? kNormBlocks : 2048;
-  pr.q_blocks = (int32_t)std::min(most, (pr.q_units + 15) / 16);
-  pr.k_blocks = (int32_t)std::min(most, (pr.k_units + 15) / 16);
-  a.q_blocks = pr.q_blocks, a.k_blocks = pr.k_blocks;
+  pr.units = row_heads(*p);
 
   hipError_t e = hipSuccess;
-  const int blocks = pr.q_blocks + pr.k_blocks;
+  // enough workgroups to fill the GPU several times
+  const int64_t blocks = std::min<int64_t>(2048, (pr.units + 15) / 16);
   if (blocks > 0)
     e = p->dtype == GS_F16 ? launch(&k_attn_prep<F16>, blocks, 256, pr, stream)
                            : launch(&k_attn_prep<BF16>, blocks, 256, pr, stream);

@@ -19,18 +19,12 @@
 
 namespace gs {
 
-// At most this many workgroups of the preparation look at norms; each writes its
-// own maximum, and the passes take the largest (no atomics, nothing to clear).
-constexpr int kNormBlocks = 512;
-
 struct AttnBwdArgs {
   AttnShape s;
   AttnArray q, k, v, dout, dq, dk, dv;
   const float* lse2;       // lse log2 e
   const float* delta;
   int64_t st_sb, st_sh;    // elements: lse2 and delta of (sequence, head)
-  const float* norms;      // fp16: largest row norms of dout and (from kNormBlocks on) v
-  int32_t q_blocks, k_blocks;  // and how many there are
   int32_t tiles, heads;    // as in AttnFwdArgs
   float c;                 // scale log2 e
   int32_t splits;          // dK, dV: workgroups that share the query heads of a key head
@@ -40,54 +34,31 @@ struct AttnBwdArgs {
 };
 
 // fp16: kernel weights enter dV times 2^15 (a weight of 2^-16, one key of 65536,
-// would be subnormal), and dS times 2^e with the largest possible |dS|, twice the
-// product of the row norms of dout and v, below 2^15; both exact, taken out of the
-// sums.  bf16 has the exponents of fp32.
+// would be subnormal), and dS times a power of two of every column's own, moved as
+// the forward pass moves its offsets: where the column's largest |dS| so far times
+// it exceeds 2^15, it is brought back to 2^13 or above and the sums are scaled with
+// it.  Both are exact and taken out of the sums.  So dS is held to 2^-38 of the
+// column's largest, whatever other columns, heads and sequences hold: an infinity or
+// NaN spoils its own columns only.  bf16 has the exponents of fp32.
 constexpr int kWeightShift = 15;
+constexpr float kDsLimit = 0x1p15f;
+constexpr int kDsExponent = 14;       // brought to [2^13, 2^14)
+constexpr float kDsFirst = 0x1p100f;
 template <typename T>
 constexpr bool scaled() { return __is_same(T, F16); }
 
-__device__ __forceinline__ int ds_exponent(const float* norms, int q_blocks, int k_blocks) {
-  // all loads at once, then their maximum
-  float x[2][kNormBlocks / 64];
-#pragma unroll
-  for (int i = 0; i < kNormBlocks / 64; ++i) {
-    const int at = i * 64 + (threadIdx.x & 63);
-    x[0][i] = at < q_blocks ? norms[at] : 0.0f;
-    x[1][i] = at < k_blocks ? norms[kNormBlocks + at] : 0.0f;
-  }
-  float z = 1.0f;
-#pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    float m = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kNormBlocks / 64; ++i) m = x[side][i] <= m ? m : x[side][i];
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const float y = __shfl_xor(m, d);
-      m = y <= m ? m : y;
-    }
-    z *= m;
-  }
-  if (!(z > 0.0f) || !(z < __builtin_inff())) return 0;
-  int e;
-  (void)frexpf(z, &e);  // z < 2^e
-  return uniform(clampi(14 - e, -100, 100));
-}
+// e with x in [2^(e-1), 2^e).
+__device__ __forceinline__ int exponent_of(float x) { return __builtin_amdgcn_frexp_expf(x); }
 
-// lse in log2 units, delta, and for fp16 the largest row norms of dout and v over
-// the rows in use.  16 lanes a row and head; bound by reading dout and out.
+// lse in log2 units and delta.  16 lanes a row and head; bound by reading dout and out.
 struct AttnPrepArgs {
   AttnShape s;
-  AttnArray out, low, dout, v;  // low.p may be NULL
+  AttnArray out, low, dout;  // low.p may be NULL
   const float* lse;
   float* lse2;
   float* delta;
   int64_t st_sb, st_sh;
-  float* norms;         // NULL: not wanted
-  int64_t q_units;      // rows x query heads, all sequences
-  int64_t k_units;      // rows x key heads (0: no norms)
-  int32_t q_blocks, k_blocks;
+  int64_t units;        // rows x query heads, all sequences
 };
 
 __device__ __forceinline__ bool row_used(const int32_t* index, int packed, int b, int i, int rows, int B) {
@@ -115,65 +86,32 @@ __device__ __forceinline__ void row8(const char* row, int vec, int width, int c,
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_prep(const AttnPrepArgs a) {
-  __shared__ float wave_max[4];
   const AttnShape& s = a.s;
   const int lane = threadIdx.x & 15;
-  const bool keys = (int)blockIdx.x >= a.q_blocks;
-  const int block = keys ? (int)blockIdx.x - a.q_blocks : (int)blockIdx.x;
-  const int64_t units = keys ? a.k_units : a.q_units, stride = (int64_t)(keys ? a.k_blocks : a.q_blocks) * 16;
-  const int H = keys ? s.Hkv : s.Hq, R = keys ? s.N : s.M;
-  float norm = 0.0f;
-  for (int64_t unit = (int64_t)block * 16 + (threadIdx.x >> 4); unit < units; unit += stride) {
-    const int h = (int)(unit % H);
-    const int64_t row = unit / H;
-    const int b = s.packed ? 0 : (int)(row / R), i = s.packed ? (int)row : (int)(row % R);
-    float dot = 0.0f, sq = 0.0f;
+  for (int64_t unit = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); unit < a.units; unit += (int64_t)gridDim.x * 16) {
+    const int h = (int)(unit % s.Hq);
+    const int64_t row = unit / s.Hq;
+    const int b = s.packed ? 0 : (int)(row / s.M), i = s.packed ? (int)row : (int)(row % s.M);
+    float dot = 0.0f;
     for (int c = 8 * lane; c < s.C; c += 128) {
-      float x[8];
-      if (keys) {
-        row8<T>(a.v.p + b * a.v.sb + i * a.v.sr + h * a.v.sh, a.v.vec, s.C, c, x);
-      } else {
-        float o[8];
-        row8<T>(a.dout.p + b * a.dout.sb + i * a.dout.sr + h * a.dout.sh, a.dout.vec, s.C, c, x);
-        row8<T>(a.out.p + b * a.out.sb + i * a.out.sr + h * a.out.sh, a.out.vec, s.C, c, o);
-        if (a.low.p) {
-          float l[8];
-          row8<T>(a.low.p + b * a.low.sb + i * a.low.sr + h * a.low.sh, a.low.vec, s.C, c, l);
+      float x[8], o[8];
+      row8<T>(a.dout.p + b * a.dout.sb + i * a.dout.sr + h * a.dout.sh, a.dout.vec, s.C, c, x);
+      row8<T>(a.out.p + b * a.out.sb + i * a.out.sr + h * a.out.sh, a.out.vec, s.C, c, o);
+      if (a.low.p) {
+        float l[8];
+        row8<T>(a.low.p + b * a.low.sb + i * a.low.sr + h * a.low.sh, a.low.vec, s.C, c, l);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += l[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(x[e], o[e], dot);
+        for (int e = 0; e < 8; ++e) o[e] += l[e];
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(x[e], x[e], sq);
+      for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(x[e], o[e], dot);
     }
 #pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-      sq += __shfl_xor(sq, d);
-      dot += __shfl_xor(dot, d);
-    }
-    if (!keys && lane == 0) {
+    for (int d = 1; d < 16; d <<= 1) dot += __shfl_xor(dot, d);
+    if (lane == 0) {
       const int64_t at = b * a.st_sb + h * a.st_sh + i;
       a.delta[at] = dot;
       a.lse2[at] = a.lse[at] * kLog2e;
-    }
-    if (a.norms && row_used(keys ? s.k_index : s.q_index, s.packed, b, i, R, s.B)) {
-      const float z = __builtin_sqrtf(sq);
-      norm = z <= norm ? norm : z;  // a NaN stays
-    }
-  }
-  if (a.norms) {
-#pragma unroll
-    for (int d = 16; d < 64; d <<= 1) {
-      const float z = __shfl_xor(norm, d);
-      norm = z <= norm ? norm : z;
-    }
-    if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = norm;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 1; w < 4; ++w) norm = wave_max[w] <= norm ? norm : wave_max[w];
-      a.norms[(keys ? kNormBlocks : 0) + block] = norm;
     }
   }
 }
@@ -294,8 +232,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       du[ct][n] = floatx4{0, 0, 0, 0};
       if (KV) dw[ct][n] = floatx4{0, 0, 0, 0};
     }
-  const int ds_e = scaled<T>() ? ds_exponent(a.norms, a.q_blocks, a.k_blocks) : 0;
-  const float ds_up = __builtin_ldexpf(1.0f, ds_e);
+  float up[NT];  // fp16: what dS is multiplied by
+#pragma unroll
+  for (int n = 0; n < NT; ++n) up[n] = scaled<T>() ? kDsFirst : 1.0f;
 
   const TileLane<DP> ln;
   // the stream: tiles of rows [r_lo, r_hi), once for every query head (KV)
@@ -447,12 +386,40 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
               }
               // the weights and dS are rounded to the inputs' type for the matrix cores
               sc[n][r] = scaled<T>() ? p * (float)(1 << kWeightShift) : p;
-              dp[n][r] = scaled<T>() ? d * ds_up : d;
+              dp[n][r] = d;
             }
             pw[n][2 * t] = pack2<T>(sc[n][0], sc[n][1]);
             pw[n][2 * t + 1] = pack2<T>(sc[n][2], sc[n][3]);
-            dsw[n][2 * t] = pack2<T>(dp[n][0], dp[n][1]);
-            dsw[n][2 * t + 1] = pack2<T>(dp[n][2], dp[n][3]);
+            if (!scaled<T>()) {
+              dsw[n][2 * t] = pack2<T>(dp[n][0], dp[n][1]);
+              dsw[n][2 * t + 1] = pack2<T>(dp[n][2], dp[n][3]);
+            }
+          }
+        }
+        if constexpr (scaled<T>()) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float mx = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, __builtin_fabsf(dp2[t][n][r]));
+            if (__any(mx * up[n] > kDsLimit)) {
+              mx = fmaxf(mx, __shfl_xor(mx, 16));
+              mx = fmaxf(mx, __shfl_xor(mx, 32));
+              // (an infinity spoils its column anyway)
+              const bool grow = mx * up[n] > kDsLimit && mx < __builtin_inff();
+              const int e = grow ? kDsExponent - exponent_of(mx) : exponent_of(up[n]) - 1;
+              const float by = __builtin_ldexpf(1.0f, e - (exponent_of(up[n]) - 1));
+              up[n] = __builtin_ldexpf(1.0f, e);
+#pragma unroll
+              for (int ct = 0; ct < NO; ++ct) du[ct][n] *= by;
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int r = 0; r < 2; ++r)
+                dsw[n][2 * t + r] = pack2<T>(dp2[t][n][2 * r] * up[n], dp2[t][n][2 * r + 1] * up[n]);
           }
         }
         uint4 pb[NT], db[NT];
@@ -480,7 +447,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       }
     }
 
-  const float u_scale = s.scale * __builtin_ldexpf(1.0f, -ds_e);
   const float w_scale = scaled<T>() ? 1.0f / (1 << kWeightShift) : 1.0f;
   const AttnArray& DU = KV ? a.dk : a.dq;
 #pragma unroll
@@ -488,13 +454,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
     const int at = wc0 + 16 * n + col;
     if (at >= limit || (at >= cn && (!(s.zero_rest & kRestOut) || split > 0))) continue;
     const bool none = at >= cn;
+    const float down = scaled<T>() ? __builtin_ldexpf(1.0f, 1 - exponent_of(up[n])) : 1.0f;
     if (KV && a.splits > 1 && !none) {
       const int64_t row = (s.packed ? 0 : (int64_t)b * s.N) + c0 + at, rows = (int64_t)(s.packed ? 1 : s.B) * s.N;
       float* p = a.part + ((split * rows + row) * s.Hkv + head) * a.part_width;
 #pragma unroll
       for (int ct = 0; ct < NO; ++ct) {
         const float nan = spoilt[n] ? __builtin_nanf("") : 0.0f;
-        store_sums(p, 16 * ct + 4 * g, s.D, du[ct][n] * u_scale + nan);
+        store_sums(p, 16 * ct + 4 * g, s.D, du[ct][n] * down * s.scale + nan);
         store_sums(p + a.part_width / 2, 16 * ct + 4 * g, s.C, dw[KV ? ct : 0][n] * w_scale + nan);
       }
       continue;
@@ -503,7 +470,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_bwd(const AttnBwdArgs a) {
       char* p = DU.p + b * DU.sb + (int64_t)(c0 + at) * DU.sr + head * DU.sh;
 #pragma unroll
       for (int ct = 0; ct < NO; ++ct) {
-        floatx4 y = du[ct][n] * u_scale;
+        floatx4 y = du[ct][n] * down * s.scale;
         if (spoilt[n]) y = floatx4{1, 1, 1, 1} * __builtin_nanf("");
         if (none) y = floatx4{0, 0, 0, 0};
         store4<T>(p, 16 * ct + 4 * g, s.D, DU.vec, y[0], y[1], y[2], y[3]);

@@ -95,3 +95,88 @@ def test_a_first_key_of_minus_infinity(at, M, dtype):
     r = ref.one(q[0, 1:], k[0, 1:], v[0, 1:], 0.125, True)
     ref.check("out", out[0, 1:], *r["out"])
     ref.check("lse", lse[0, :, 1:], *r["lse"])
+
+
+def check_sequence(name, grads, q, k, v, g, scale, some=(), **kw):
+    r = ref.one(q, k, v, scale, dout=g, **kw)
+    for n, t in zip(("dq", "dk", "dv"), grads):
+        val, bound = r[n]
+        if t.dtype == torch.float16:
+            # from 65520 on, half a step above its largest number, fp16 rounds to infinity: right where the
+            # exact value is there, give or take its bound
+            over = (t.cpu() == val.sign() * math.inf) & (val.abs() + bound >= 65520)
+            val = torch.where(over, t.cpu().double(), val)
+        ref.check("%s of %s" % (n, name), t, val, bound)
+        assert n not in some or t.any(), "%s of %s is 0" % (n, name)
+
+
+# dS of 4e-8, less than a step of fp16, while the gradient named first is of ordinary size: standard
+# deviations of q and k, with scores of about 1 at a scale of 100
+SMALL = {"dq": (1e-4, 10.0), "dk": (10.0, 1e-4)}
+
+
+def small(seed, some, B, M, N, Hq, Hkv, D, dtype):
+    gen = torch.Generator().manual_seed(seed)
+    std = SMALL[some]
+    return (normal(gen, (B, M, Hq, D), dtype, std[0]), normal(gen, (B, N, Hkv, D), dtype, std[1]),
+            normal(gen, (B, N, Hkv, D), dtype), normal(gen, (B, M, Hq, D), dtype, 1e-5))
+
+
+@pytest.mark.parametrize("some", ["dq", "dk"])
+@pytest.mark.parametrize("where", ["dout", "v"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, 3e4])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_small_gradients_beside_another_sequence(at, some, where, bad, dtype):
+    """dS far below what 16 bits hold beside a sequence with numbers that are large or not finite: dense, and
+    packed with shared heads."""
+    for Hq, Hkv, D in ((2, 2, 64), (4, 1, 128)):
+        q, k, v, g = small(41, some, 2, 70, 2000, Hq, Hkv, D, dtype)
+        {"dout": g, "v": v}[where][1, 9, :, 3] = bad
+        out, lse = at.attention_fwd(q, k, v, scale=100.0)
+        grads = at.attention_bwd(q, k, v, out, lse, g, scale=100.0)
+        check_sequence("the dense sequence", [t[0] for t in grads], q[0], k[0], v[0], g[0], 100.0, some)
+        pk = [t.flatten(0, 1) for t in (q, k, v, g)]
+        offs = [torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda") for n in (70, 2000)]
+        out, lse = at.attention_fwd(*pk[:3], scale=100.0, q_offsets=offs[0], k_offsets=offs[1])
+        grads = at.attention_bwd(*pk[:3], out, lse, pk[3], scale=100.0, q_offsets=offs[0], k_offsets=offs[1])
+        check_sequence("the packed sequence", (grads[0][:70], grads[1][:2000], grads[2][:2000]), q[0], k[0], v[0], g[0],
+                       100.0, some)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_large_gradients_beside_a_bad_sequence(at, dtype):
+    """dS past fp16's largest number (few keys, gradients of 2e4) beside a sequence that is not finite."""
+    q, k, v, g = make(42, 2, 90, 3, 2, 2, 64, 64, dtype, std=0.1, g_std=1.5e4)
+    k *= 0.1
+    g.clamp_(-6e4, 6e4)
+    g[1, 4, 1, 7] = math.inf
+    out, lse = at.attention_fwd(q, k, v, scale=0.05)
+    grads = at.attention_bwd(q, k, v, out, lse, g, scale=0.05)
+    x = torch.matmul(g[0].cpu().double().transpose(0, 1), v[0].cpu().double().permute(1, 2, 0).contiguous()).abs().max()
+    assert x > 3 * 65504                       # (so dS, a third of it, is beyond fp16)
+    check_sequence("the finite sequence", [t[0] for t in grads], q[0], k[0], v[0], g[0], 0.05)
+
+
+@pytest.mark.parametrize("some", ["dq", "dk"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_a_bad_value_that_no_row_sees_leaves_small_gradients(at, some, bad, dtype):
+    """A window over the last keys: the first value, not finite, is seen by no row."""
+    q, k, v, g = small(43, some, 1, 70, 900, 2, 1, 64, dtype)
+    v[0, 0] = bad
+    kw = dict(causal=True, window=800)
+    out, lse = at.attention_fwd(q, k, v, scale=100.0, **kw)
+    grads = at.attention_bwd(q, k, v, out, lse, g, scale=100.0, **kw)
+    v[0, 0] = 0
+    check_sequence("the sequence", [t[0] for t in grads], q[0], k[0], v[0], g[0], 100.0, some, **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_gradients_that_grow_along_the_rows(at, dtype):
+    """dout 2^-14 in the first rows and 2^12 in the last: what dK and dV sum up grows all the way."""
+    q, k, v, g = make(44, 1, 300, 150, 4, 2, 64, 64, dtype, g_std=1.0)
+    g *= torch.exp2(torch.arange(300, device="cuda") / 300 * 26 - 14).to(dtype).view(1, 300, 1, 1)
+    for turned in (g, g.flip(1)):
+        out, lse = at.attention_fwd(q, k, v)
+        grads = at.attention_bwd(q, k, v, out, lse, turned)
+        check_sequence("the sequence", [t[0] for t in grads], q[0], k[0], v[0], turned[0], 0.125)
