@@ -54,9 +54,9 @@ struct AttnFwdArgs {
 constexpr float kOffsetBelow = 7.0f;
 constexpr float kOffsetLimit = 15.0f;
 constexpr float kNoOffset = -3.0e38f;
-// Offset of a part that holds no key of the row (one whose scores are all -inf keeps
-// kNoOffset: the row is no empty one, and its result is 0 / 0).
-constexpr float kNoKeys = -__builtin_inff();
+// The offset that a row starts with, and keeps, where it sees no key.  (One whose
+// scores are all -inf keeps kNoOffset: it is no empty row, and its result is 0 / 0.)
+constexpr float kNoKeys = -3.2e38f;
 
 __device__ __forceinline__ int page_index(const AttnPages& pg, int j) {
   return pg.shift >= 0 ? j >> pg.shift : (int)((uint32_t)j / (uint32_t)pg.size);
@@ -344,7 +344,7 @@ struct AttnRows {
   int lo[NQ], hi[NQ];      // keys that the row sees
   uint4 q[NQ][NC];
   floatx4 o[NO][NQ];       // sums of weights times values
-  float off[NQ], sum[NQ];  // offset of the exponents, sum of the weights in this lane
+  float off[NQ], sum[NQ];  // offset of the exponents (start_offsets), sum of the weights in this lane
 
   // Rows wr0 ..; rows past the end repeat the last one (nothing of them is written).
   __device__ __forceinline__ void start(const AttnFwdArgs& a, const AttnJob& w, int wr0) {
@@ -355,7 +355,6 @@ struct AttnRows {
       const int token = a.per > 1 ? r / a.per : r;
       const int h = a.per > 1 ? w.head * a.per + (r - token * a.per) : w.head;
       lo[n] = hi[n] = 0;
-      off[n] = kNoOffset;
       sum[n] = 0.0f;
 #pragma unroll
       for (int ct = 0; ct < NO; ++ct) o[ct][n] = floatx4{0, 0, 0, 0};
@@ -366,6 +365,12 @@ struct AttnRows {
         for (int c = 0; c < NC; ++c) q[n][c] = column_operand<T>(p, a.q.vec, a.s.D, c, a.neg);
       }
     }
+  }
+
+  // Where the offsets start: the keys of this workgroup are [from, to).
+  __device__ __forceinline__ void start_offsets(int from, int to) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) off[n] = max(lo[n], from) < min(hi[n], to) ? kNoOffset : kNoKeys;
   }
 
   // The keys key0 .. of a tile, H steps of 32.  masked: some row does not see all
@@ -452,17 +457,14 @@ struct AttnRows {
     }
   }
   int max_key;  // the last key whose page number is at hand
-
-  // Whether the row of column tile n sees any of the keys [from, to).
-  __device__ __forceinline__ bool sees(int n, int from, int to) const { return max(lo[n], from) < min(hi[n], to); }
 };
 
-// Results of columns c .. c + 3 of row r (o / sum of weights z, offset off; seen: the
-// row sees keys here; first: the thread that writes the row's own numbers): to the
-// caller's arrays, or as part of a row whose keys are split.
+// Results of columns c .. c + 3 of row r (o / sum of weights z, offset off; first:
+// the thread that writes the row's own numbers): to the caller's arrays, or as
+// part of a row whose keys are split.
 template <typename T>
 __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w, int r, int c, floatx4 o, float off,
-                                          float z, bool seen, bool first) {
+                                          float z, bool first) {
   const AttnShape& s = a.s;
   if (r >= w.limit) return;
   const bool rest = r >= w.rows;
@@ -472,12 +474,12 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
   const int64_t row = w.sq.q0 + token;
   if (a.splits > 1) {
     const int64_t at = ((w.part * (int64_t)(s.packed ? 1 : s.B) + (s.packed ? 0 : w.b)) * s.M + row) * s.Hq + h;
-    if (first) a.part_z[2 * at] = seen ? off : kNoKeys, a.part_z[2 * at + 1] = z;
-    if (!seen) return;  // the sums are not looked at
+    if (first) a.part_z[2 * at] = off, a.part_z[2 * at + 1] = z;
+    if (off == kNoKeys) return;  // the sums are not looked at
     store_sums(a.part_o + at * s.C, c, s.C, o);
     return;
   }
-  const bool empty = rest || !seen;
+  const bool empty = rest || off == kNoKeys;
   const float inv = 1.0f / z;
   floatx4 y;
 #pragma unroll
@@ -513,6 +515,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
   const KeyRange mine = keys_of_rows(a, job, wr0, wr0 + 16 * NQ - 1);
   int k_lo = all.lo, k_hi = all.hi;
   split_keys(a, job, BK, k_lo, k_hi);
+  rows.start_offsets(k_lo, k_hi);
 
   const TileLane<DP> ln;
   const char* kb = a.k.p + (PAGED ? 0 : job.b * a.k.sb + (int64_t)job.sq.k0 * a.k.sr) + job.kvh * a.k.sh;
@@ -583,7 +586,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnFwdArgs a) {
       floatx4 y = rows.o[ct][n];
       if (infinities) add_infinities<NB>(inf_bits[threadIdx.x], n, ct, y);
       write_row<T>(a, job, wr0 + 16 * n + (lane & 15), 16 * ct + 4 * (lane >> 4), y, rows.off[n], z,
-                   rows.sees(n, k_lo, k_hi), ct == 0 && lane < 16);
+                   ct == 0 && lane < 16);
     }
   }
 }
@@ -600,7 +603,6 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
   __shared__ uint32_t inf_bits[NT][2 * NQ * NB];
   __shared__ int32_t slice[PAGED ? kSlice : 1];
   __shared__ float w_off[NW][ROWS], w_sum[NW][ROWS];
-  __shared__ bool seen[ROWS];
   const AttnShape& s = a.s;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 
@@ -612,6 +614,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
   const KeyRange all = keys_of_rows(a, job, job.r0, job.r0 + ROWS - 1);
   int k_lo = all.lo, k_hi = all.hi;
   split_keys(a, job, 32, k_lo, k_hi);
+  rows.start_offsets(k_lo, k_hi);
 
   const TileLane<DP> ln;
   const char* kb = a.k.p + (PAGED ? 0 : job.b * a.k.sb + (int64_t)job.sq.k0 * a.k.sr) + job.kvh * a.k.sh;
@@ -671,13 +674,12 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
     z += __shfl_xor(z, 16);
     z += __shfl_xor(z, 32);
     if (lane < 16) w_off[wave][16 * n + lane] = rows.off[n], w_sum[wave][16 * n + lane] = z;
-    if (threadIdx.x < 16) seen[16 * n + lane] = rows.sees(n, k_lo, k_hi);
   }
   __syncthreads();  // also: every wave is done with its ring
   floatx4* join = reinterpret_cast<floatx4*>(smem);
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    float top = kNoOffset;
+    float top = kNoKeys;
 #pragma unroll
     for (int w = 0; w < NW; ++w) top = fmaxf(top, w_off[w][16 * n + (lane & 15)]);
     const float by = __builtin_amdgcn_exp2f(rows.off[n] - top);
@@ -691,7 +693,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
   __syncthreads();
   for (int i = threadIdx.x; i < NQ * NO * 64; i += NT) {
     const int l = i & 63, n = i / (NO * 64), ct = (i >> 6) % NO, r = 16 * n + (l & 15);
-    float top = kNoOffset, z = 0.0f;
+    float top = kNoKeys, z = 0.0f;
     floatx4 y{0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < NW; ++w) top = fmaxf(top, w_off[w][r]);
@@ -700,7 +702,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_rows(const AttnFwdArgs a) {
       z += w_sum[w][r] * __builtin_amdgcn_exp2f(w_off[w][r] - top);
       y += join[w * NQ * NO * 64 + i];
     }
-    write_row<T>(a, job, job.r0 + r, 16 * ct + 4 * (l >> 4), y, top, z, seen[r], ct == 0 && l < 16);
+    write_row<T>(a, job, job.r0 + r, 16 * ct + 4 * (l >> 4), y, top, z, ct == 0 && l < 16);
   }
 }
 
