@@ -456,6 +456,15 @@ __device__ __forceinline__ void store4(char* row, int c, int width, int vec, flo
   }
 }
 
+// A row's result, which lies between its smallest and largest value: the weights'
+// own rounding can bring it past fp16's largest number by up to 2^-11 of it, and from
+// 2^-12 on it would round to infinity.
+template <typename T>
+__device__ __forceinline__ float between(float y) {
+  constexpr float most = 65504.0f;
+  return __is_same(T, F16) && __builtin_fabsf(y) < __builtin_inff() ? fminf(fmaxf(y, -most), most) : y;
+}
+
 // What rounding x to T leaves.
 template <typename T>
 __device__ __forceinline__ float left(float x) {

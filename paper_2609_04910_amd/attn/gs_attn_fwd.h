@@ -483,7 +483,7 @@ __device__ __forceinline__ void write_row(const AttnFwdArgs& a, const AttnJob& w
   const float inv = 1.0f / z;
   floatx4 y;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : o[e] * inv;
+  for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : between<T>(o[e] * inv);
   if (!rest || (s.zero_rest & kRestOut)) {
     store4<T>(a.out.p + w.b * a.out.sb + row * a.out.sr + h * a.out.sh, c, s.C, a.out.vec, y[0], y[1], y[2], y[3]);
     if (a.low.p)
@@ -765,7 +765,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnFwdArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], d);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : y[e] * inv;
+  for (int e = 0; e < 4; ++e) y[e] = empty ? 0.0f : between<T>(y[e] * inv);
   if (group == 0) {
     store4<T>(out, c, s.C, a.out.vec, y[0], y[1], y[2], y[3]);
     if (low) store4<T>(low, c, s.C, a.low.vec, left<T>(y[0]), left<T>(y[1]), left<T>(y[2]), left<T>(y[3]));

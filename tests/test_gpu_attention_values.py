@@ -180,3 +180,21 @@ def test_gradients_that_grow_along_the_rows(at, dtype):
         out, lse = at.attention_fwd(q, k, v)
         grads = at.attention_bwd(q, k, v, out, lse, turned)
         check_sequence("the sequence", [t[0] for t in grads], q[0], k[0], v[0], turned[0], 0.125)
+
+
+@pytest.mark.parametrize("N", [900, 4000])
+def test_values_at_the_largest_number(at, N):
+    """Every value is fp16's largest number, so every result is.  The weights of most keys are rounded up
+    (128 exp(0.00052) = 128.067 to 128.125), which brings the sums past 65520, where fp16 has infinity."""
+    q = torch.zeros((1, 70, 1, 64), dtype=torch.float16, device="cuda")
+    k = torch.zeros((1, N, 1, 64), dtype=torch.float16, device="cuda")
+    q[..., 0] = 1
+    k[:, 64:, :, 0] = 0.00052
+    v = torch.full((1, N, 1, 64), 65504.0, dtype=torch.float16, device="cuda")
+    v[..., 1] = -65504.0
+    low = torch.empty_like(q)
+    out, _ = at.attention_fwd(q, k, v, scale=1.0, low=low)
+    assert torch.equal(out, v[:, :1].expand(1, 70, 1, 64)) and low.isfinite().all()
+    v[0, 9, 0, 2] = math.inf                   # an infinity stays one
+    out, _ = at.attention_fwd(q, k, v, scale=1.0)
+    assert (out[..., 2] == math.inf).all() and out[..., 3:].isfinite().all()
