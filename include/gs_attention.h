@@ -91,7 +91,8 @@ typedef struct {
  * the keys at k.data + x * k.batch_stride.  lens: keys of each sequence, those of
  * the call's own tokens included.  A key on a page whose number is outside
  * [0, pages) reads as NaN and is not written; positions from table_width *
- * page_size on do not exist, nor does any in a cache of 0 pages. */
+ * page_size on do not exist (they are not written and not seen; the tokens of a
+ * longer sequence keep their places), nor does any in a cache of 0 pages. */
 typedef struct {
   gs_attention_array k, v;
   int64_t pages, page_size, table_width;

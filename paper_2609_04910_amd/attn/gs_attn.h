@@ -151,7 +151,8 @@ __device__ __forceinline__ int folded(int id, int blocks) {
 }
 
 // Rows that column point `at` (its index in its sequence) sees on the other
-// side: [lo, hi).  ahead = keys - queries.  Queries see keys up to their own
+// side: [lo, hi).  ahead: place of the first query among the keys (keys - queries,
+// or more where the keys end with a page table).  Queries see keys up to their own
 // place (causal) and the last `window` of them; keys are seen the other way
 // round.
 __device__ __forceinline__ void query_range(const AttnShape& s, int at, int ahead, int kn, int& lo, int& hi) {
@@ -159,7 +160,7 @@ __device__ __forceinline__ void query_range(const AttnShape& s, int at, int ahea
   if (s.causal) {
     const int end = at + ahead + 1;  // may be negative: nothing seen
     hi = clampi(end, 0, kn);
-    if (s.window > 0 && end > s.window) lo = end - s.window;  // lo <= end, and hi = min(end, kn)
+    if (s.window > 0 && end > s.window) lo = end - s.window;  // may lie past the keys: nothing seen
     lo = lo > hi ? hi : lo;
   }
 }

@@ -225,6 +225,7 @@ __device__ __forceinline__ void add_infinities(const uint32_t (&bits)[NB2], int 
 struct AttnJob {
   int b, kvh, head;    // head: the first of the `per` query heads of the rows, over per
   AttnSeq sq;
+  int ahead;           // place of the first query among the keys (causal)
   int rows, limit;     // rows of the sequence (token-major, then its query heads), and rows that the call owns
   int r0;              // first row of the tile
   int part;            // which split
@@ -299,11 +300,15 @@ __device__ __forceinline__ bool attn_job(const AttnFwdArgs& a, AttnJob& w) {
       w.sq.q0 = 0, w.sq.qn = s.M;
     w.sq.q0 = uniform(w.sq.q0), w.sq.qn = uniform(w.sq.qn);
     w.sq.k0 = 0;
-    // a cache without pages holds no keys
+    // a cache without pages holds no keys; where a sequence is longer than its table
+    // has room for, its tokens keep their places and the keys end with the table
     const int64_t room = a.pg.pages > 0 ? (int64_t)a.pg.width * a.pg.size : 0;
-    w.sq.kn = uniform(clampi(a.pg.lens[w.b], 0, (int)min(room, (int64_t)0x3fffffff)));
+    const int len = uniform(max(a.pg.lens[w.b], 0));
+    w.sq.kn = min(len, (int)min(room, (int64_t)0x3fffffff));
+    w.ahead = len - w.sq.qn;
   } else {
     w.sq = seq_of(s, w.b);
+    w.ahead = w.sq.kn - w.sq.qn;
   }
   w.rows = w.sq.qn * a.per;
   w.limit = s.packed ? w.rows : s.M * a.per;
@@ -318,9 +323,8 @@ struct KeyRange {
 __device__ __forceinline__ KeyRange keys_of_rows(const AttnFwdArgs& a, const AttnJob& w, int first, int last) {
   KeyRange r;
   if (first >= w.rows) return r;
-  const int ahead = w.sq.kn - w.sq.qn;
-  query_range(a.s, first / a.per, ahead, w.sq.kn, r.lo, r.in_hi);
-  query_range(a.s, min(last, w.rows - 1) / a.per, ahead, w.sq.kn, r.in_lo, r.hi);
+  query_range(a.s, first / a.per, w.ahead, w.sq.kn, r.lo, r.in_hi);
+  query_range(a.s, min(last, w.rows - 1) / a.per, w.ahead, w.sq.kn, r.in_lo, r.hi);
   return r;
 }
 
@@ -359,7 +363,7 @@ struct AttnRows {
 #pragma unroll
       for (int ct = 0; ct < NO; ++ct) o[ct][n] = floatx4{0, 0, 0, 0};
       if (w.rows > 0) {
-        query_range(a.s, token, w.sq.kn - w.sq.qn, w.sq.kn, lo[n], hi[n]);
+        query_range(a.s, token, w.ahead, w.sq.kn, lo[n], hi[n]);
         const char* p = a.q.p + w.b * a.q.sb + (int64_t)(w.sq.q0 + token) * a.q.sr + h * a.q.sh;
 #pragma unroll
         for (int c = 0; c < NC; ++c) q[n][c] = column_operand<T>(p, a.q.vec, a.s.D, c, a.neg);

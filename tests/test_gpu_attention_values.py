@@ -198,3 +198,24 @@ def test_values_at_the_largest_number(at, N):
     v[0, 9, 0, 2] = math.inf                   # an infinity stays one
     out, _ = at.attention_fwd(q, k, v, scale=1.0)
     assert (out[..., 2] == math.inf).all() and out[..., 3:].isfinite().all()
+
+
+@pytest.mark.parametrize("rows", [1, 10, 100])
+@pytest.mark.parametrize("window", [0, 6, 90])
+def test_lengths_past_the_table_keep_every_tokens_place(at, rows, window):
+    """A length beyond the table's room: its keys end there, and a token still sees up to its own
+    place (where attention_append puts it), not further back."""
+    gen = torch.Generator().manual_seed(47)
+    k, v = normal(gen, (160, 1, 64), torch.bfloat16), normal(gen, (160, 1, 64), torch.bfloat16)
+    q = normal(gen, (rows, 2, 64), torch.bfloat16)
+    kp, vp, table, lens = paged_of(k, v)
+    for n in (161, 165, 170, 300, 2 ** 31 - 1):
+        lens.fill_(n)
+        out, lse = at.attention_paged(q, kp, vp, table, lens, window=window, return_lse=True)
+        place, key = torch.arange(rows).unsqueeze(1) + (n - rows), torch.arange(160).unsqueeze(0)
+        see = key <= place
+        if window:
+            see &= key > place - window
+        r = ref.one(q, k, v, 0.125, see=see)
+        ref.check("out", out, *r["out"])
+        ref.check("lse", lse, *r["lse"])
