@@ -54,7 +54,7 @@ hipError_t launch(K kernel, int64_t grid, int threads, const A& args, hipStream_
 }
 
 // rows: rows of a tile; few: k_attn_rows (16 or rows_most(DP)), else k_attn_fwd
-// (attn_fwd_rows(DP) or attn_less_rows(DP))
+// (attn_fwd_rows(DP) or, not over pages, attn_less_rows(DP))
 template <typename T, int DP>
 hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, bool few, int rows, int64_t grid, hipStream_t st);
 // cols: columns of a workgroup, attn_bwd_cols(DP, kv) or (not DP = 256) half of them
@@ -68,13 +68,10 @@ hipError_t attn_rows(const AttnFwdArgs& a, int64_t grid, hipStream_t st) {
   return launch(a.k.vec && a.v.vec ? &k_attn_rows<T, DP, NQ, NW, PAGED, true> : &k_attn_rows<T, DP, NQ, NW, PAGED, false>,
                 grid, 64 * NW, a, st);
 }
-template <typename T, int DP, int NQ>
-hipError_t attn_tiles(const AttnFwdArgs& a, bool paged, int64_t grid, hipStream_t st) {
+template <typename T, int DP, int NQ, bool PAGED>
+hipError_t attn_tiles(const AttnFwdArgs& a, int64_t grid, hipStream_t st) {
   constexpr int NW = kAttnWaves;
-  const bool wide = a.k.vec && a.v.vec;
-  return launch(paged ? wide ? &k_attn_fwd<T, DP, NQ, NW, true, true> : &k_attn_fwd<T, DP, NQ, NW, true, false>
-                : wide ? &k_attn_fwd<T, DP, NQ, NW, false, true>
-                       : &k_attn_fwd<T, DP, NQ, NW, false, false>,
+  return launch(a.k.vec && a.v.vec ? &k_attn_fwd<T, DP, NQ, NW, PAGED, true> : &k_attn_fwd<T, DP, NQ, NW, PAGED, false>,
                 grid, 64 * NW, a, st);
 }
 template <typename T, int DP>
@@ -86,8 +83,9 @@ hipError_t attn_fwd(const AttnFwdArgs& a, bool paged, bool few, int rows, int64_
         : paged    ? attn_rows<T, DP, MOST, true>(a, grid, st)
                    : attn_rows<T, DP, MOST, false>(a, grid, st);
   } else {
-    e = rows == attn_less_rows(DP) ? attn_tiles<T, DP, attn_less_nq(DP)>(a, paged, grid, st)
-                                   : attn_tiles<T, DP, attn_nq(DP)>(a, paged, grid, st);
+    e = paged                        ? attn_tiles<T, DP, attn_nq(DP), true>(a, grid, st)
+        : rows == attn_less_rows(DP) ? attn_tiles<T, DP, attn_less_nq(DP), false>(a, grid, st)
+                                     : attn_tiles<T, DP, attn_nq(DP), false>(a, grid, st);
   }
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t units = (int64_t)(a.s.packed ? 1 : a.s.B) * a.s.M * a.s.Hq;
