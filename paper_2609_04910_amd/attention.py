@@ -205,7 +205,7 @@ def _check_stream(stream, device):
 
 class _Call:
     """Checked sizes of a forward or backward call."""
-    __slots__ = ("sizes", "modes", "scale", "packed", "index", "out_shape", "lse_shape", "gpu")
+    __slots__ = ("sizes", "modes", "scale", "packed", "index", "out_shape", "lse_shape", "gpu", "grad")
 
     def __init__(self, q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens):
         qs, ks, vs = q.shape, k.shape, v.shape
@@ -397,7 +397,9 @@ def _make_autograd():
     class Attention(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, v, call):
-            low = torch.empty(call.out_shape, dtype=q.dtype, device=q.device) if any(ctx.needs_input_grad) else None
+            # needs_input_grad tells of the inputs, also where no graph is made (call.grad)
+            want_low = call.grad and any(ctx.needs_input_grad)
+            low = torch.empty(call.out_shape, dtype=q.dtype, device=q.device) if want_low else None
             out, lse = _fwd(call, q, k, v, None, None, low, None, None)
             ctx.save_for_backward(q, k, v, out, lse, low, *(t for t in call.index if t is not None))
             ctx.call = call
@@ -426,10 +428,12 @@ _autograd = None
 
 def attention(q, k, v, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None, q_lens=None, k_lens=None):
     """attention_fwd under autograd: out, with gradients for q, k and v (arguments as there)."""
+    import torch
     global _autograd
     if _autograd is None:
         _autograd = _make_autograd()
     c = _Call(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+    c.grad = torch.is_grad_enabled()
     return _autograd.apply(q, k, v, c)
 
 
