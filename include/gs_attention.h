@@ -130,7 +130,8 @@ size_t gs_attention_bwd_workspace_size(const gs_attention_problem* p, int want_d
  * their keys and values already (gs_attention_append): token i of qn sees the
  * keys up to its own position lens[b] - qn + i (causal has to be 1; N is not
  * used).  q and out: packed, or dense with M tokens of every sequence (q_index
- * NULL).  lse: Hq x (rows of all sequences), or NULL. */
+ * NULL).  lse: Hq x (rows of all sequences), or NULL.  M == 0, or B == 0 in the
+ * dense layout, is a no-op. */
 gs_status gs_attention_paged(const gs_attention_problem* p, const gs_attention_array* q,
                              const gs_attention_cache* cache, const int32_t* q_index,
                              const gs_attention_array* out, float* lse, void* workspace,

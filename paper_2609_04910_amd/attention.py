@@ -542,19 +542,9 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
         if return_lse:
             lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
             rest |= REST_LSE
-        if sizes[0] == 0:  # no sequences: every row is one of none
-            if rest & REST_OUT:
-                out.zero_()
-            if lse is not None:
-                lse.fill_(float("-inf"))
-        else:
-            need = _paged_bytes(sizes, modes, k_pages.shape[1], page_table.shape[1])
-            if need or workspace is not None:
-                workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
-    if sizes[0] == 0:
-        if stream is not None:
-            gs._keep_alive(stream, out, lse)
-        return (out, lse) if return_lse else out
+        need = _paged_bytes(sizes, modes, k_pages.shape[1], page_table.shape[1])
+        if need or workspace is not None:
+            workspace, wbytes = gs._workspace_arg(workspace, need, q.device)
     buf, at = _buffer()
     _PACK_PAGED(buf, 0, *sizes, *modes, rest, D ** -0.5 if scale is None else float(scale),
                 *_row_numbers(q, sizes, modes), *_row_numbers(out, sizes, modes),

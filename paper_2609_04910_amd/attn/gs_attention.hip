@@ -527,7 +527,7 @@ gs_status cache_of(const gs_attention_problem& p, const gs_attention_cache* c, b
   if (c->pages < 0 || c->pages > kMaxRows || c->page_size < 1 || c->page_size > kMaxRows || c->table_width < 0 ||
       c->table_width > kMaxRows || (c->table_width > 0 && c->page_size > kMaxRows / c->table_width))
     return GS_ERR_BAD_SHAPE;
-  if (!c->lens || (c->table_width > 0 && !c->table)) return GS_ERR_NULL_POINTER;
+  if (p.B > 0 && (!c->lens || (c->table_width > 0 && !c->table))) return GS_ERR_NULL_POINTER;
   if ((reinterpret_cast<uintptr_t>(c->lens) | reinterpret_cast<uintptr_t>(c->table)) & 3) return GS_ERR_MISALIGNED;
   gs_status st = array_of(&c->k, c->pages, c->page_size, p.Hkv, p.D, output, k, ks);
   if (st == GS_SUCCESS) st = array_of(&c->v, c->pages, c->page_size, p.Hkv, p.C, output, v, vs);
@@ -556,7 +556,7 @@ gs_status run_paged(const gs_attention_problem* p, const gs_attention_array* q, 
   gs_status st = check(p);
   if (st != GS_SUCCESS) return st;
   if (!p->causal) return GS_ERR_UNSUPPORTED;
-  if (p->B == 0 || p->M == 0) return GS_SUCCESS;
+  if ((p->B == 0 && !p->packed) || p->M == 0) return GS_SUCCESS;
   if (p->packed ? !q_index : q_index != nullptr) return p->packed ? GS_ERR_NULL_POINTER : GS_ERR_UNSUPPORTED;
   if (reinterpret_cast<uintptr_t>(q_index) & 3) return GS_ERR_MISALIGNED;
   const int64_t B = p->packed ? 1 : p->B, G = p->Hq / p->Hkv;
@@ -650,7 +650,7 @@ gs_status gs_attention_bwd(const gs_attention_problem* p, const gs_attention_arr
 }
 
 size_t gs_attention_paged_workspace_size(const gs_attention_problem* p, const gs_attention_cache* cache) {
-  if (gs::check(p) != GS_SUCCESS || !cache || p->B == 0 || p->M == 0 || cache->table_width < 0 ||
+  if (gs::check(p) != GS_SUCCESS || !cache || (p->B == 0 && !p->packed) || p->M == 0 || cache->table_width < 0 ||
       cache->page_size < 1 || cache->page_size > gs::kMaxRows || cache->table_width > gs::kMaxRows)
     return 0;
   return gs::fwd_plan(*p, true, gs::cache_keys(*cache), nullptr).total;
