@@ -73,3 +73,31 @@ def test_gauss_sums():
     batched = [t.expand(3, -1, -1).contiguous() for t in (q, k, v, g)]
     run(lambda st: gs.gauss_sum_fwd_bwd_batched(*batched[:3], 0.1, batched[3], stream=st),
         gs.gauss_sum_fwd_bwd_batched_workspace_size(700, 900, 32, 4, 3))
+
+
+def test_a_call_on_a_stream_forked_in_a_capture():
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v = (torch.randn((2, n, 2, 64), generator=gen, device="cuda").half() for n in (60, 5000, 5000))
+    g = torch.randn(q.shape, generator=gen, device="cuda").half()
+    side = torch.cuda.Stream()
+
+    def step(stream):
+        out, lse = at.attention_fwd(q, k, v, stream=stream)
+        return (out, lse) + at.attention_bwd(q, k, v, out, lse, g, stream=stream)
+
+    want = [t.clone() for t in step(None)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        held = step(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for t in held:
+            t.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b)
+        step(None)
+        torch.cuda.synchronize()
