@@ -199,7 +199,7 @@ def _check_call(q, k, v, causal, window, q_offsets, k_offsets, q_lens, k_lens):
 
 def _check_stream(stream, device):
     """A kernel enqueued on another GPU's stream would run there, on this one's addresses."""
-    if stream is not None and stream.device != device:
+    if stream.device != device:
         raise ValueError("stream must be on %s, got one on %s" % (device, stream.device))
 
 
@@ -297,7 +297,8 @@ def _check_like_out(t, name, c, q):
 
 def _fwd(c, q, k, v, out, lse, low, workspace, stream):
     import torch
-    _check_stream(stream, q.device)
+    if stream is not None:
+        _check_stream(stream, q.device)
     rest = 0
     if out is not None:
         _check_like_out(out, "out", c, q)
@@ -355,7 +356,8 @@ def attention_bwd_workspace_size(B, M, N, Hq, Hkv, D, C, dtype=gs.GS_F16, packed
 
 def _bwd(c, q, k, v, out, lse, dout, want, low, workspace, stream):
     import torch
-    _check_stream(stream, q.device)
+    if stream is not None:
+        _check_stream(stream, q.device)
     want = int(bool(want[0])), int(bool(want[1])), int(bool(want[2]))
     with gs._HERE if stream is None else gs._on(stream):
         dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want[0] else None
@@ -502,7 +504,8 @@ def attention_append(k, v, k_pages, v_pages, page_table, seq_lens, q_offsets=Non
     if sizes[4] != H:
         raise ValueError("k has %d heads, the pages have %d" % (H, sizes[4]))
     _check_gpu(("k", k), ("v", v), ("k_pages", k_pages), ("v_pages", v_pages))
-    _check_stream(stream, k.device)
+    if stream is not None:
+        _check_stream(stream, k.device)
     buf, at = _buffer()
     _PACK_PAGED(buf, 0, *sizes, *modes, 0, 1.0, *_row_numbers(k, sizes, modes), *_row_numbers(v, sizes, modes),
                 *_cache_numbers(k_pages, v_pages, page_table, seq_lens))
@@ -530,7 +533,8 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     C = v_pages.shape[3]
     sizes, modes = _cache_call(q, "q", k_pages, v_pages, page_table, seq_lens, q_offsets, Hq, D, C, code, window)
     _check_gpu(("q", q), ("k_pages", k_pages), ("v_pages", v_pages))
-    _check_stream(stream, q.device)
+    if stream is not None:
+        _check_stream(stream, q.device)
     rest, lse, wbytes = 0, None, 0
     if out is not None:
         _check_out(out, "out", (T, Hq, C), q.dtype, q.device)
