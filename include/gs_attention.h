@@ -45,7 +45,11 @@
  *     `zero_rest` asks, written as 0 (out and gradients) and -inf (lse).
  *   - The library allocates nothing; the workspace (256-byte aligned, its
  *     contents ignored and left undefined) is the caller's.  Calls that may
- *     overlap in time need workspaces of their own.
+ *     overlap in time need workspaces of their own.  That of the backward pass
+ *     holds 8 bytes a query row and head, and, where few keys leave the query heads
+ *     of a key head to s workgroups (s at most Hq / Hkv), s sums of 8 max(D, C)
+ *     bytes a key and key head: 268 MB for 8192 tokens, 32 heads over 8, D = 128,
+ *     causal.
  *
  * Execution: as in gauss_sum.h.  All work is enqueued on `stream`, arguments are
  * validated before anything is enqueued, nothing synchronises, the calls may be
@@ -56,8 +60,10 @@
  * Products run on the matrix cores with fp32 sums; scores, exponentials, their sums
  * and lse are fp32.  Weights (relative to the row's maximum), and P and dS of the
  * backward pass, are rounded once to the inputs' type before they are contracted,
- * and results once at the end.  NaN and Inf propagate to the rows that see them
- * and to no other.
+ * and results once at the end; in fp16 P and dS enter times powers of two, dS times
+ * one of each row's (dK: key's) own.  Sums of weights (below 2^15) times values are
+ * fp32, so bf16 values beyond 2^112 may overflow.  NaN and Inf propagate to the rows
+ * that see them and to no other.
  */
 #ifndef GS_ATTENTION_H
 #define GS_ATTENTION_H
@@ -100,7 +106,10 @@ typedef struct {
   const int32_t* lens;
 } gs_attention_cache;
 
-/* out and (unless NULL) lse of every row.  low (unless NULL): what the rounding
+/* All calls: GS_ERR_BAD_SHAPE also where a launch would need more than 2^24 - 1
+ * workgroups (tiles of rows times heads and sequences).
+ *
+ * out and (unless NULL) lse of every row.  low (unless NULL): what the rounding
  * of out leaves, out - rounded, itself rounded to the dtype, for the backward
  * pass.  M == 0, or B == 0 in the dense layout, is a no-op.
  * Workspace: gs_attention_fwd_workspace_size(p) bytes (which may be 0). */

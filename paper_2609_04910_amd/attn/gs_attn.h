@@ -208,9 +208,13 @@ typedef __attribute__((address_space(3))) char attn_lds;
 __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(const attn_lds*)p; }
 
 // 64 lanes x 16 (4) bytes from base + per-lane offset, or from per-lane
-// addresses, to LDS bytes lds + 16 (4) * lane.  Assembly, so that the compiler
-// neither sees nor waits for the copy: the tile loop waits (tile_barrier) before the
-// barrier that publishes it.  The s_nop separates the write of m0 from its use.
+// addresses, to LDS bytes lds + 16 (4) * lane.  Assembly, so that the compiler does
+// not count the copy: the tile loop waits (copies_done) before the barrier that
+// publishes it.  The compiler's waits for its own loads take the copies in all the
+// same: where operands loaded before a tile loop are first used inside it (the query
+// operands of the forward kernels, the columns' of dK and dV where they are in
+// registers), it waits there in every tile, and so for most or all of the next
+// tile's copies.  The s_nop separates the write of m0 from its use.
 __device__ __forceinline__ void copy16(const char* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :

@@ -454,8 +454,8 @@ struct AttnRows {
           sum[n] += x[t][n][r];
         }
       // weights rounded to the values' type (the matrix cores take nothing
-      // wider): at most 2^-9 (bf16) or 2^-12 (fp16) of each; the sum of weights
-      // is of the unrounded ones
+      // wider): at most half a step, 2^-8 (bf16) or 2^-11 (fp16) of each; the sum of
+      // weights is of the unrounded ones
       w[n] = uint4{pack2<T>(x[0][n][0], x[0][n][1]), pack2<T>(x[0][n][2], x[0][n][3]),
                    pack2<T>(x[1][n][0], x[1][n][1]), pack2<T>(x[1][n][2], x[1][n][3])};
     }
