@@ -324,7 +324,7 @@ def gauss_sum_fwd(q, k, v, tau, out=None, workspace=None, stream=None):
     p = make_problem(M, N, D, C, _dtype_code(q.dtype), _dtype_code(v.dtype))
     lib = load()
     need = int(lib.gauss_sum_fwd_workspace_size(ctypes.byref(p)))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         out = _output(out, "out", (M, C), q.device)
         workspace, wbytes = _workspace_arg(workspace, need, q.device)
     st = lib.gauss_sum_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), float(tau), _ptr(out),
@@ -369,7 +369,7 @@ def gauss_sum_bwd(q, k, v, tau, dout, want=(True, True, True), workspace=None, s
     dev = q.device
     need = int(lib.gauss_sum_bwd_workspace_size(ctypes.byref(p), int(bool(want[0])),
                                                 int(bool(want[1])), int(bool(want[2]))))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         dq = torch.empty((M, D), dtype=torch.float32, device=dev) if want[0] else None
         dk = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
         dv = torch.empty((N, C), dtype=torch.float32, device=dev) if want[2] else None
@@ -397,7 +397,7 @@ def gauss_sum_fwd_bwd(q, k, v, tau, dout, want=(True, True, True), out=None, wor
     dev = q.device
     need = int(lib.gauss_sum_fwd_bwd_workspace_size(ctypes.byref(p), int(bool(want[0])),
                                                     int(bool(want[1])), int(bool(want[2]))))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         out = _output(out, "out", (M, C), dev)
         dq = torch.empty((M, D), dtype=torch.float32, device=dev) if want[0] else None
         dk = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
@@ -460,7 +460,7 @@ def gauss_sum_fwd_batched(q, k, v, tau, out=None, workspace=None, stream=None, g
     lib = load()
     b = Batch(B, qs, ks, vs, 0, M * C, 0, 0, 0)
     need = int(lib.gauss_sum_fwd_batched_workspace_size(ctypes.byref(p), int(group or max(B, 1))))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         out = _output(out, "out", (B, M, C), q.device)
         workspace, wbytes = _workspace_arg(workspace, need, q.device)
     st = lib.gauss_sum_fwd_batched(ctypes.byref(p), ctypes.byref(b), _ptr(q), _ptr(k), _ptr(v),
@@ -489,7 +489,7 @@ def gauss_sum_bwd_batched(q, k, v, tau, dout, want=(True, True, True), workspace
     need = int(lib.gauss_sum_bwd_batched_workspace_size(ctypes.byref(p), int(group or max(B, 1)),
                                                         int(bool(want[0])), int(bool(want[1])),
                                                         int(bool(want[2]))))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         dq = torch.empty((B, M, D), dtype=torch.float32, device=dev) if want[0] else None
         dk = torch.empty((B, N, D), dtype=torch.float32, device=dev) if want[1] else None
         dv = torch.empty((B, N, C), dtype=torch.float32, device=dev) if want[2] else None
@@ -528,7 +528,7 @@ def gauss_sum_fwd_bwd_batched(q, k, v, tau, dout, want=(True, True, True), out=N
     need = int(lib.gauss_sum_fwd_bwd_batched_workspace_size(ctypes.byref(p), int(group or max(B, 1)),
                                                             int(bool(want[0])), int(bool(want[1])),
                                                             int(bool(want[2]))))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         out = _output(out, "out", (B, M, C), dev)
         dq = torch.empty((B, M, D), dtype=torch.float32, device=dev) if want[0] else None
         dk = torch.empty((B, N, D), dtype=torch.float32, device=dev) if want[1] else None
@@ -562,7 +562,7 @@ def gauss_sum_mmd_flow(x, v, tau, want=(True, True, True), workspace=None, strea
     lib = load()
     dev = x.device
     need = int(lib.gauss_sum_mmd_flow_workspace_size(ctypes.byref(p)))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         s = torch.empty((N, 1), dtype=torch.float32, device=dev) if want[0] else None
         grad = torch.empty((N, D), dtype=torch.float32, device=dev) if want[1] else None
         mmd2 = torch.empty((), dtype=torch.float64, device=dev) if want[2] else None
@@ -593,7 +593,7 @@ def gauss_sum_svgd(x, score, tau, out=None, workspace=None, stream=None):
     lib = load()
     dev = x.device
     need = int(lib.gauss_sum_svgd_workspace_size(ctypes.byref(p)))
-    with _on(stream):
+    with _HERE if stream is None else _on(stream):
         out = _output(out, "out", (N, D), dev)
         workspace, wbytes = _workspace_arg(workspace, need, dev)
     st = lib.gauss_sum_svgd(ctypes.byref(p), _ptr(x), _ptr(score), float(tau), _ptr(out), _ptr(workspace),
