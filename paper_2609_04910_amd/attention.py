@@ -22,7 +22,11 @@ fp16 or bf16, results in the inputs' dtype, lse (log sum exp of the scores) in
 fp32 as B x Hq x M or Hq x T.
 
 Rows that belong to no sequence are 0 (lse: -inf) in results allocated here and
-left as they were in the caller's own (out=, lse=).
+left as they were in the caller's own (out=, lse=; low= goes with out).
+
+stream=: the call's kernels go to that stream of the tensors' GPU, and its results
+and workspace are allocated there.  Inputs have to be ready on it, and other streams
+wait for it before they read the results.
 """
 import ctypes
 import functools
@@ -523,7 +527,8 @@ def attention_paged(q, k_pages, v_pages, page_table, seq_lens, q_offsets=None, s
     cache that holds their keys and values already (attention_append; arguments as there):
     token i of the qn new ones of sequence b sees the keys up to its own position,
     seq_lens[b] - qn + i, with window > 0 the last `window` of them.  Returns out (T x Hq x C), or
-    (out, lse) with lse Hq x T.  A row that sees a key whose page number lies outside the cache is NaN."""
+    (out, lse) with lse Hq x T.  A row that sees a key whose page number lies outside the cache is NaN;
+    positions behind the table's last page hold no key."""
     import torch
     _check_columns("q", q, 3)
     if not (isinstance(v_pages, torch.Tensor) and v_pages.dim() == 4):

@@ -17,6 +17,7 @@ Entry points mirror the C names:
   gauss_sum_fwd_batched / gauss_sum_bwd_batched (B independent problems,
   grid.z) and their workspace sizes; gauss_sum_mmd_flow (s, flow field, MMD^2)
   gauss_sum_status_string / gauss_sum_abi_version
+A call with stream= allocates its results and workspace on that stream.
 and ``GaussSum`` wraps both in a torch.autograd.Function.
 """
 import contextlib
